@@ -54,8 +54,11 @@ enum {
     SD_STATUS_POOL_FULL = 2,      /* the slot's node pool or text buffer ran full;    */
                                   /* its tree stopped growing at the last good token  */
     SD_STATUS_GLOBAL_FULL = 4,    /* the global node pool ran full during an insert   */
-    SD_STATUS_BAD_TOKEN = 8       /* a token outside [0, V) was met; the tree stopped */
+    SD_STATUS_BAD_TOKEN = 8,      /* a token outside [0, V) was met; the tree stopped */
                                   /* growing at the last good token                   */
+    SD_STATUS_BAD_ROWS = 16,      /* sd_rotate ... sd_commit: the request's rows, its */
+                                  /* length or its path make no sense; left out       */
+    SD_STATUS_BAD_PAGE = 32       /* a page outside the cache was met                 */
 };
 
 /* sd_spec_params.flags */
@@ -265,6 +268,147 @@ int sd_speculate_noalloc(sd_store* store, int32_t n, const int32_t* d_slot, cons
                          const int32_t* d_budget_cap, int32_t* d_n_draft, int32_t* d_tokens,
                          int32_t* d_parents, int32_t* d_positions, uint32_t* d_mask, int32_t* d_chosen_tree,
                          int32_t* d_chosen_p, double* d_score, int32_t* d_status, void* stream);
+
+/*
+ * ---- The verifier's side of a step ------------------------------------------------------------
+ *
+ * A draft tree is verified by one pass of the model over the rows [last token, draft nodes] of every request
+ * (Section 3: the drafts are verified with tree attention under the mask of sd_speculate).  The four calls below are
+ * what that pass needs beside its matrix products, on the arrays that sd_speculate writes and sd_step reads:
+ *
+ *     sd_speculate -> [ per layer: sd_rotate, sd_attend ] -> sd_accept -> sd_commit -> sd_step
+ *
+ * Rows of the batch are packed: request i has the rows d_offsets[i] .. d_offsets[i+1) of every row array, row 0 of
+ * them the request's last token and row j + 1 its draft node j, so 1 + n_draft[i] rows; none for a slot that idles.
+ * While it is verified, row r lies at place d_cached[i] + r of the request's cache; its position in the sequence is
+ * d_cached[i] + (number of bits set in its mask row) (0 for row 0), that is the cached tokens and its ancestors.
+ *
+ * The cache is paged: place p of request i is line p % page_size of page d_table[i][p / page_size].  A cache that is
+ * one piece per request is one whose pages have the length of a request (table_stride 1).
+ *
+ * The calls allocate nothing, copy nothing to or from the host and may be captured into a graph.  They keep nothing
+ * between calls and share nothing, so calls on different streams do not meet as long as their buffers do not.  What
+ * depends on device data is told per request in d_status (SD_STATUS_*, written by every call; may be NULL).  A request whose numbers make
+ * no sense (offsets that descend or leave the row arrays, more rows than 1 + max_draft, a negative length, places
+ * beyond its table) gets SD_STATUS_BAD_ROWS, and its rows stay as they were.  Of a page outside the cache nothing is
+ * read or written, and the request gets SD_STATUS_BAD_PAGE; rows that should have seen it hold nothing of use.  Row arrays
+ * may be longer than d_offsets[n]: rows behind it are not touched.
+ */
+enum { SD_BF16 = 1, SD_FP16 = 2, SD_FP32 = 3 };
+
+typedef struct {
+    void* d_k;                    /* keys and values of line 0 of page 0, head 0 (layer 0)   */
+    void* d_v;
+    int32_t dtype;                /* SD_BF16 or SD_FP16                               */
+    int32_t kv_heads;
+    int32_t head_dim;             /* 64 or 128; the elements of a head are adjacent   */
+    int32_t n_layers;             /* sd_commit; else 1                                */
+    int32_t n_pages;
+    int32_t page_size;            /* 8, 16, 32, 64 or a multiple of 128; any size     */
+                                  /* where table_stride is 1                          */
+    int64_t k_stride[4];          /* elements from layer to layer, page to page, line */
+    int64_t v_stride[4];          /* to line, head to head: > 0, multiples of 8       */
+} sd_cache;
+
+typedef struct {
+    int32_t n;                    /* requests                                         */
+    int32_t rows;                 /* length of the row arrays                         */
+    int32_t max_draft;            /* 0 .. 64: M, row stride of d_mask                 */
+    int32_t table_stride;         /* pages per request in d_table                     */
+    const int64_t* d_offsets;     /* int64[n + 1]                                     */
+    const int32_t* d_cached;      /* int32[n]: tokens of the request in the cache     */
+    const int32_t* d_table;       /* int32[n][table_stride]                           */
+    const uint32_t* d_mask;       /* uint32[n][M][(M+31)/32] as sd_speculate writes   */
+                                  /* it, or NULL: each row sees all rows before it    */
+    int32_t* d_status;            /* int32[n] or NULL                                 */
+} sd_rows;
+
+typedef struct {
+    int32_t q_heads;              /* a multiple of kv_heads: q_heads / kv_heads       */
+                                  /* consecutive ones share a head of the cache       */
+    int32_t rot_dim;              /* the first rot_dim elements of a head are turned: */
+                                  /* a multiple of 16, <= head_dim, 0: none           */
+    int32_t interleaved;          /* pairs (2j, 2j + 1); else (j, j + rot_dim / 2)    */
+    float scale;                  /* factor of the turned elements (long contexts)    */
+    float eps;                    /* of the norms                                     */
+    int64_t q_stride[2], k_stride[2], v_stride[2], out_stride[2];   /* elements from row to row, head to head: multiples of 8 */
+} sd_rotate_params;
+
+typedef struct {
+    int32_t q_heads;
+    float scale;                  /* factor of the scores, usually 1 / sqrt(head_dim) */
+    int32_t window;               /* a row at position x sees positions > x - window; */
+                                  /* 0: all                                           */
+    int32_t sinks;                /* ... and always the positions below this          */
+    int32_t shared;               /* the first `shared` places of all requests are in */
+                                  /* the same pages (one prompt for all): their keys  */
+                                  /* are read once for the batch.  0 .. every         */
+                                  /* d_cached[i] of a request with rows               */
+    int64_t q_stride[2], out_stride[2];     /* elements from row to row, head to head: multiples of 8 */
+} sd_attend_params;
+
+/*
+ * sd_rotate: queries, keys and values of the rows as a projection left them, made ready for sd_attend in one pass:
+ *   x' = x / sqrt(mean(x^2) + eps) * weight   for queries and keys, over a head; left out where its weight is NULL
+ *   (a, b) -> scale * (a cos - b sin, b cos + a sin)   for the pairs j of the first rot_dim elements,
+ *                                             by the angle position * d_freq[j]
+ * and keys and values written to the rows' places in the cache.  Computed in 32 bits (the angle in 64) and rounded once.
+ *   d_q, d_k, d_v  [rows][heads][head_dim] in the cache's dtype, by their strides
+ *   d_freq         double[rot_dim / 2]: radians per position
+ *   d_positions    int32[rows] or NULL: the rows' positions, if they are not those given above
+ *   d_q_weight, d_k_weight  [head_dim] in the cache's dtype, or NULL
+ *   d_q_out        [rows][q_heads][head_dim]; may be d_q with the same strides
+ * Errors: INVALID_ARG, CUDA.
+ */
+int sd_rotate(const sd_cache* cache, const sd_rows* rows, const sd_rotate_params* params, const void* d_q, const void* d_k,
+              const void* d_v, const double* d_freq, const int32_t* d_positions, const void* d_q_weight,
+              const void* d_k_weight, void* d_q_out, void* stream);
+
+/*
+ * sd_attend: attention of the rows over their requests' caches.  Row r of request i sees
+ *   - place p < d_cached[i] (position p), and
+ *   - of the rows of its own request, row 0 and those whose bit is set in its mask row (its ancestors and itself),
+ * each only if its position is inside the row's window or below `sinks`.  out = softmax(scale * q k) v over these;
+ * 0 for a row that sees nothing.  Scores, softmax and sums are 32 bits; weights are rounded to the cache's type
+ * for the product with the values.  What a row does not see has no part in its result, whatever it holds (NaN too).
+ *   d_q, d_out   [rows][q_heads][head_dim], by their strides; d_out may be d_q with the same strides
+ *   d_lse        float[rows][q_heads] or NULL: log of the sum of exp(score), -inf for a row that sees nothing
+ *   d_workspace  sd_attend_workspace() bytes, 256-byte aligned, undefined before and after; a call needs one of its own as long as it runs
+ * Errors: INVALID_ARG, CAPACITY (workspace too small), CUDA.
+ */
+int sd_attend(const sd_cache* cache, const sd_rows* rows, const sd_attend_params* params, const void* d_q, void* d_out,
+              float* d_lse, void* d_workspace, int64_t workspace_bytes, void* stream);
+
+/* sd_attend_workspace: bytes of d_workspace for such a call on the current device; negative: SD_ERR_*. */
+int64_t sd_attend_workspace(const sd_cache* cache, const sd_rows* rows, const sd_attend_params* params);
+
+/*
+ * sd_accept: greedy verification.  The model's choice at a row is the vocabulary entry of its largest logit (the
+ * lowest index of equal ones; NaN counts as larger than every number).  From row 0 on, the draft node that is a
+ * child of the row and has the row's choice as its token is accepted, until there is none; siblings carry different
+ * tokens (as those of sd_speculate do; of equal ones the lowest index is taken).  The choices along the path are the
+ * request's new tokens: the accepted drafts and one more.  Section 4.1's simulated verifier does the same on the host.
+ *   dtype            of the logits: SD_BF16, SD_FP16 or SD_FP32
+ *   d_logits         [rows][vocab], row_stride elements from row to row
+ *   d_offsets        int64[n + 1]; d_tokens, d_parents int32[n][max_draft] as sd_speculate writes them
+ *   d_targets        int32[rows]: every row's choice (rows behind d_offsets[n] as well)
+ *   d_path           int32[n][max_draft + 1]: rows of the accepted path, row 0 first, -1 beyond
+ *   d_new_offsets    int64[n + 1], d_new_tokens int32[rows]: arguments of sd_step; d_new_tokens is -1 beyond d_new_offsets[n]
+ *   d_status         int32[n] or NULL
+ * Errors: INVALID_ARG, CUDA.
+ */
+int sd_accept(int32_t n, int32_t rows, int32_t max_draft, int32_t vocab, int32_t dtype, int64_t row_stride, const void* d_logits,
+              const int64_t* d_offsets, const int32_t* d_tokens, const int32_t* d_parents, int32_t* d_targets, int32_t* d_path,
+              int64_t* d_new_offsets, int32_t* d_new_tokens, int32_t* d_status, void* stream);
+
+/*
+ * sd_commit: the keys and values of the accepted rows stay in the cache: line d_cached[i] + d_path[i][j] goes to line
+ * d_cached[i] + j, in every layer, and d_new_cached[i] = d_cached[i] + rows of the path (the request's length from now
+ * on; may be d_cached).  d_path as sd_accept writes it: ascending, -1 behind the last row.
+ * Of `rows` n, max_draft, table_stride, d_cached, d_table and d_status are used.
+ * Errors: INVALID_ARG, CUDA.
+ */
+int sd_commit(const sd_cache* cache, const sd_rows* rows, const int32_t* d_path, int32_t* d_new_cached, void* stream);
 
 /*
  * sd_query_counts: COUNT of arbitrary token paths (the quantity Eq. 1 divides),

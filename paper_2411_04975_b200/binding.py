@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import importlib.util
+import math
 import os
 import subprocess
 import warnings
@@ -21,10 +22,11 @@ from . import build as _build
 
 FLAG_GLOBAL_ONLY, FLAG_REQUEST_ONLY, FLAG_LINEAR = 1, 2, 4
 STATUS_BAD_SLOT, STATUS_POOL_FULL, STATUS_GLOBAL_FULL, STATUS_BAD_TOKEN = 1, 2, 4, 8
+STATUS_BAD_ROWS, STATUS_BAD_PAGE = 16, 32
 
 EXPORTS = ["sd_build", "sd_build_requests", "sd_append", "sd_speculate", "sd_step", "sd_speculate_noalloc", "sd_query_counts",
            "sd_enumerate", "sd_slot_info", "sd_entropy", "sd_stats", "sd_free", "sd_trim", "sd_strerror", "sd_debug_fail_alloc",
-           "sd_debug_small_clusters"]
+           "sd_debug_small_clusters", "sd_rotate", "sd_attend", "sd_attend_workspace", "sd_accept", "sd_commit"]
 
 
 class SuffixSpecError(RuntimeError):
@@ -49,6 +51,30 @@ class _Stats(C.Structure):
                 ("global_tokens", C.c_int64), ("slot_pool_nodes", C.c_int64), ("device_bytes", C.c_int64),
                 ("global_status", C.c_int32)]
 
+
+class _Cache(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("dtype", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("n_layers", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("k_stride", C.c_int64 * 4),
+                ("v_stride", C.c_int64 * 4)]
+
+
+class _Rows(C.Structure):
+    _fields_ = [("n", C.c_int32), ("rows", C.c_int32), ("max_draft", C.c_int32), ("table_stride", C.c_int32), ("d_offsets", C.c_void_p),
+                ("d_cached", C.c_void_p), ("d_table", C.c_void_p), ("d_mask", C.c_void_p), ("d_status", C.c_void_p)]
+
+
+class _RotateParams(C.Structure):
+    _fields_ = [("q_heads", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_float), ("eps", C.c_float),
+                ("q_stride", C.c_int64 * 2), ("k_stride", C.c_int64 * 2), ("v_stride", C.c_int64 * 2), ("out_stride", C.c_int64 * 2)]
+
+
+class _AttendParams(C.Structure):
+    _fields_ = [("q_heads", C.c_int32), ("scale", C.c_float), ("window", C.c_int32), ("sinks", C.c_int32), ("shared", C.c_int32),
+                ("q_stride", C.c_int64 * 2), ("out_stride", C.c_int64 * 2)]
+
+
+MAX_DRAFT = 64
+_DTYPES = {torch.bfloat16: 1, torch.float16: 2, torch.float32: 3}
 
 _lib = None
 _call = None               # the module of the per-step calls; loaded with the library
@@ -94,6 +120,17 @@ def library() -> C.CDLL:
         lib.sd_debug_fail_alloc.argtypes = [C.c_int64]
         lib.sd_debug_small_clusters.restype = None
         lib.sd_debug_small_clusters.argtypes = [C.c_int32]
+        cache, rows = C.POINTER(_Cache), C.POINTER(_Rows)
+        lib.sd_rotate.restype = C.c_int
+        lib.sd_rotate.argtypes = [cache, rows, C.POINTER(_RotateParams)] + [vp] * 9
+        lib.sd_attend.restype = C.c_int
+        lib.sd_attend.argtypes = [cache, rows, C.POINTER(_AttendParams), vp, vp, vp, vp, C.c_int64, vp]
+        lib.sd_attend_workspace.restype = C.c_int64
+        lib.sd_attend_workspace.argtypes = [cache, rows, C.POINTER(_AttendParams)]
+        lib.sd_accept.restype = C.c_int
+        lib.sd_accept.argtypes = [C.c_int32] * 5 + [C.c_int64] + [vp] * 10
+        lib.sd_commit.restype = C.c_int
+        lib.sd_commit.argtypes = [cache, rows, vp, vp, vp]
         lib.sd_strerror.restype = C.c_char_p
         lib.sd_strerror.argtypes = [C.c_int]
         _lib, _call = lib, _load_call(lib)
@@ -111,6 +148,8 @@ def _load_call(lib):
         call = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(call)
         call.setup(*(C.cast(f, C.c_void_p).value for f in (lib.sd_speculate, lib.sd_step, lib.sd_append)), _ptr)
+        call.setup_verifier(*(C.cast(f, C.c_void_p).value for f in (lib.sd_rotate, lib.sd_attend, lib.sd_attend_workspace,
+                                                                    lib.sd_accept, lib.sd_commit)))
         return call
     except (ImportError, OSError, subprocess.CalledProcessError) as e:
         warnings.warn(f"the native module of the per-step calls could not be had ({e}): each call takes the host some 6 us longer",
@@ -119,7 +158,7 @@ def _load_call(lib):
 
 
 class _PlainCall:
-    """speculate, step and append of the module _call through ctypes."""
+    """The calls of the module _call through ctypes."""
 
     def __init__(self, lib):
         self._lib = lib
@@ -139,6 +178,120 @@ class _PlainCall:
         return self._lib.sd_append(
             store, int(slots.numel()), _ptr(slots, torch.int32, "slots"), _ptr(offsets, torch.int64, "offsets"),
             _ptr(tokens, torch.int32, "tokens"), _ptr(reset, torch.uint8, "reset"), _stream())
+
+
+    def rotate(self, q, k, v, k_cache, v_cache, table, offsets, cached, freq, mask, positions, q_weight, k_weight, eps, interleaved,
+               scale, out, status) -> int:
+        cache, dt = _cache_of(k_cache, v_cache, (4,)), k_cache.dtype
+        rows, n = _length(q, "q"), _length(offsets, "offsets") - 1
+        b = _rows_of(rows, table, offsets, cached, mask, status)
+        heads, D = _q_heads(q), k_cache.shape[-1]
+        if heads > 65536 or freq.numel() > 64:
+            raise TypeError("rotate: at most 65,536 heads and 64 frequencies")
+        strides = [_heads(t, dt, (rows, h, D), name) for t, h, name in ((q, heads, "q"), (k, cache.kv_heads, "k"), (v, cache.kv_heads, "v"), (out, heads, "out"))]
+        p = _RotateParams(heads, 2 * freq.numel(), int(interleaved), scale, eps, *strides)
+        return self._lib.sd_rotate(
+            C.byref(cache), C.byref(b), C.byref(p), q.data_ptr(), k.data_ptr(), v.data_ptr(), _array(freq, torch.float64, (freq.numel(),), "freq"),
+            _array(positions, torch.int32, (rows,), "positions"), _array(q_weight, dt, (D,), "q_weight"),
+            _array(k_weight, dt, (D,), "k_weight"), out.data_ptr(), _stream())
+
+    def attend(self, q, k_cache, v_cache, table, offsets, cached, mask, scale, window, sinks, shared, out, lse, status) -> int:
+        cache, dt = _cache_of(k_cache, v_cache, (4,)), k_cache.dtype
+        rows = _length(q, "q")
+        b = _rows_of(rows, table, offsets, cached, mask, status)
+        heads, D = _q_heads(q), k_cache.shape[-1]
+        for name, x in (("q_heads", heads), ("window", window), ("sinks", sinks), ("shared", shared)):
+            if not 0 <= x <= (65536 if name == "q_heads" else 0x7FFFFFFF):
+                raise SuffixSpecError(-1, f"sd_attend: {name} {x}")
+        p = _AttendParams(heads, scale, window, sinks, shared, _heads(q, dt, (rows, heads, D), "q"), _heads(out, dt, (rows, heads, D), "out"))
+        lse = _array(lse, torch.float32, (rows, heads), "lse")
+        size = self._lib.sd_attend_workspace(C.byref(cache), C.byref(b), C.byref(p))
+        if size < 0:
+            return size
+        work = torch.empty(size, dtype=torch.uint8, device=q.device)
+        return self._lib.sd_attend(C.byref(cache), C.byref(b), C.byref(p), q.data_ptr(), out.data_ptr(), lse, work.data_ptr(), size, _stream())
+
+    def accept(self, logits, offsets, tokens, parents, targets, path, new_offsets, new_tokens, status) -> int:
+        if logits.dim() != 2 or tokens.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+            raise TypeError("accept: expected logits [rows, vocab] with adjacent entries and tokens [n, max_draft]")
+        (rows, vocab), (n, M) = logits.shape, tokens.shape
+        if logits.dtype not in _DTYPES or M > MAX_DRAFT or max(rows, vocab, n) > 0x7FFFFFFE:
+            raise TypeError(f"accept: logits of {logits.dtype}, drafts of {M}")
+        _here(logits, "logits")
+        args = [_array(t, dt, shape, name) for t, dt, shape, name in (
+            (offsets, torch.int64, (n + 1,), "offsets"), (tokens, torch.int32, (n, M), "tokens"), (parents, torch.int32, (n, M), "parents"),
+            (targets, torch.int32, (rows,), "targets"), (path, torch.int32, (n, M + 1), "path"), (new_offsets, torch.int64, (n + 1,), "new_offsets"),
+            (new_tokens, torch.int32, (rows,), "new_tokens"), (status, torch.int32, (n,), "status"))]
+        return self._lib.sd_accept(n, rows, M, vocab, _DTYPES[logits.dtype], logits.stride(0) if rows > 1 else vocab, logits.data_ptr(), *args, _stream())
+
+    def commit(self, k_cache, v_cache, table, cached, path, new_cached, status) -> int:
+        cache = _cache_of(k_cache, v_cache, (4, 5))
+        if path.dim() != 2 or not 1 <= path.shape[1] <= MAX_DRAFT + 1 or table.dim() != 2:
+            raise TypeError("commit: expected a path [n, max_draft + 1] and a table [n, pages]")
+        n, M1 = path.shape
+        b = _Rows(n, 0, M1 - 1, table.shape[1], None, _array(cached, torch.int32, (n,), "cached"),
+                  _array(table, torch.int32, (n, table.shape[1]), "table"), None, _array(status, torch.int32, (n,), "status"))
+        return self._lib.sd_commit(C.byref(cache), C.byref(b), _array(path, torch.int32, (n, M1), "path"),
+                                   _array(new_cached, torch.int32, (n,), "new_cached"), _stream())
+
+
+def _here(t: torch.Tensor, name: str) -> None:
+    if not (t.is_cuda and t.device.index == _current_device()) and not t.is_pinned():
+        raise TypeError(f"{name}: expected a tensor on the current CUDA device (or in pinned host memory), got one on {t.device}")
+
+
+def _array(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, name: str) -> Optional[int]:
+    if t is not None and tuple(t.shape) != shape:
+        raise TypeError(f"{name}: expected the shape {shape}, got {tuple(t.shape)}")
+    p = _ptr(t, dtype, name)
+    if t is not None:
+        _here(t, name)
+    return p
+
+
+def _length(t: torch.Tensor, name: str) -> int:
+    if t.dim() < 1:
+        raise TypeError(f"{name}: expected rows")
+    return t.shape[0]
+
+
+def _q_heads(q: torch.Tensor) -> int:
+    if q.dim() != 3:
+        raise TypeError(f"q: expected [rows, q_heads, head_dim], got {tuple(q.shape)}")
+    return q.shape[1]
+
+
+def _heads(t: torch.Tensor, dtype: torch.dtype, shape: tuple, name: str):
+    """Strides of rows of heads whose elements are adjacent."""
+    if t.dtype != dtype or tuple(t.shape) != shape or t.stride(2) != 1:
+        raise TypeError(f"{name}: expected {dtype} of the shape {shape} with adjacent elements, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+    _here(t, name)
+    return (C.c_int64 * 2)(t.stride(0), t.stride(1))
+
+
+def _cache_of(k: torch.Tensor, v: torch.Tensor, dims: tuple) -> _Cache:
+    if k.dtype != v.dtype or k.dtype not in _DTYPES or k.shape != v.shape or k.dim() not in dims or k.stride(-1) != 1 or v.stride(-1) != 1:
+        raise TypeError("k_cache, v_cache: expected two alike tensors [pages, page_size, kv_heads, head_dim] (sd_commit: or one per layer before "
+                        f"that) with adjacent elements, got {k.dtype} {tuple(k.shape)} and {v.dtype} {tuple(v.shape)}")
+    _here(k, "k_cache")
+    _here(v, "v_cache")
+    layers = k.dim() == 5
+    st = [(C.c_int64 * 4)(t.stride(0) if layers else 0, t.stride(-4), t.stride(-3), t.stride(-2)) for t in (k, v)]
+    return _Cache(k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], k.shape[-2], k.shape[-1], k.shape[0] if layers else 1, k.shape[-4], k.shape[-3], *st)
+
+
+def _rows_of(rows: int, table, offsets, cached, mask, status) -> _Rows:
+    n = _length(offsets, "offsets") - 1
+    if n < 0 or table.dim() != 2:
+        raise TypeError("offsets: expected one more than requests; table: expected [n, pages]")
+    M = MAX_DRAFT
+    if mask is not None:
+        if mask.dim() != 3 or mask.shape[1] > MAX_DRAFT:
+            raise TypeError(f"mask: expected [n, max_draft <= {MAX_DRAFT}, words], got {tuple(mask.shape)}")
+        M = mask.shape[1]
+    return _Rows(n, rows, M, table.shape[1], _array(offsets, torch.int64, (n + 1,), "offsets"), _array(cached, torch.int32, (n,), "cached"),
+                 _array(table, torch.int32, (n, table.shape[1]), "table"),
+                 _array(mask, torch.int32, (n, M, (M + 31) // 32), "mask"), _array(status, torch.int32, (n,), "status"))
 
 
 def _ptr(t: Optional[torch.Tensor], dtype: torch.dtype, name: str) -> Optional[int]:
@@ -218,6 +371,86 @@ def sd_speculate_noalloc(store: int, slots: torch.Tensor, P: int, alpha: float, 
         C.byref(_SpecParams(P, alpha, max_spec, flags, tau)), _ptr(budget_cap, torch.int32, "budget_cap"), *_out_ptrs(out), _stream())
     if rc != 0:
         raise SuffixSpecError(rc, "sd_speculate_noalloc")
+
+
+def _made(name: str, args: tuple) -> None:
+    """The native call, or, where one of its tensors is not usual, the same call in Python; raises what its status says."""
+    rc = getattr(_call or _loaded(), name)(*args)
+    if rc is None:
+        rc = getattr(_PlainCall(library()), name)(*args)
+    if rc != 0:
+        raise SuffixSpecError(rc, "sd_" + name)
+
+
+def sd_rotate(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
+              offsets: torch.Tensor, cached: torch.Tensor, freq: torch.Tensor, *, mask: Optional[torch.Tensor] = None,
+              positions: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+              eps: float = 1e-6, interleaved: bool = False, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+              status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Queries q [rows, q_heads, head_dim], normed (where they have a weight) and turned to the rows' positions; keys likewise and values go to the
+    rows' places in the cache [pages, page_size, kv_heads, head_dim].  freq: float64, radians per position of each pair (see
+    rotary_frequencies); the first 2 * len(freq) elements of a head are turned.  offsets, cached, table, mask: the batch (see suffixspec.h).  out may be q."""
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _made("rotate", (q, k, v, k_cache, v_cache, table, offsets, cached, freq, mask, positions, q_weight, k_weight, eps, interleaved, scale, out, status))
+    return out
+
+
+def sd_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, offsets: torch.Tensor, cached: torch.Tensor,
+              *, mask: Optional[torch.Tensor] = None, scale: Optional[float] = None, window: int = 0, sinks: int = 0, shared: int = 0,
+              out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the rows q [rows, q_heads, head_dim] of draft trees over their requests' caches under the mask of sd_speculate (None: each row
+    sees those before it).  scale: 1 / sqrt(head_dim) unless given.  window, sinks: a row sees the last `window` positions and the first `sinks` (0: all).
+    shared: so many first places of all requests are in the same pages and are read once for the batch."""
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if scale is None:
+        scale = q.shape[-1] ** -0.5
+    _made("attend", (q, k_cache, v_cache, table, offsets, cached, mask, scale, window, sinks, shared, out, lse, status))
+    return out
+
+
+def sd_accept(logits: torch.Tensor, offsets: torch.Tensor, tokens: torch.Tensor, parents: torch.Tensor, *,
+              out: Optional[Dict[str, torch.Tensor]] = None, status: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
+    """Greedy verification of the drafts (tokens, parents: of sd_speculate) against logits [rows, vocab].  Returns targets [rows], path [n, max_draft + 1],
+    and offsets [n + 1] and tokens [rows], which sd_step takes as they are."""
+    if out is None:
+        (n, M), rows, i32 = tokens.shape, logits.shape[0], dict(dtype=torch.int32, device=logits.device)
+        out = {"targets": torch.empty(rows, **i32), "path": torch.empty(n, M + 1, **i32),
+               "offsets": torch.empty(n + 1, dtype=torch.int64, device=logits.device), "tokens": torch.empty(rows, **i32)}
+    _made("accept", (logits, offsets, tokens, parents, out["targets"], out["path"], out["offsets"], out["tokens"], status))
+    return out
+
+
+def sd_commit(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, cached: torch.Tensor, path: torch.Tensor, *,
+              out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Keys and values of the accepted rows (path: of sd_accept) to where their sequences continue, in a cache
+    [pages, page_size, kv_heads, head_dim] or, for all layers at once, [layers, pages, ...].  Returns the requests' lengths from now on; out may be cached."""
+    if out is None:
+        out = torch.empty(cached.shape, dtype=cached.dtype, device=cached.device)
+    _made("commit", (k_cache, v_cache, table, cached, path, out, status))
+    return out
+
+
+def rotary_frequencies(rot_dim: int, base: float = 10000.0, *, device=None, factor: float = 1.0, original: int = 0, fast: float = 32.0,
+                       slow: float = 1.0) -> tuple:
+    """(freq, scale) for sd_rotate: base ** (-2 j / rot_dim) radians per position for pair j.  For contexts longer than a model was trained with,
+    `factor` times as long: all frequencies divided by `factor` (original = 0), or, with `original` the length it was trained with, only
+    those that turn less than `slow` times within it, none of those that turn more than `fast` times, the others in between in proportion
+    (linear in j), and the turned elements times 1 + 0.1 ln(factor)."""
+    j = torch.arange(rot_dim // 2, dtype=torch.float64)
+    freq = base ** (-2.0 * j / rot_dim)
+    scale = 1.0
+    if factor != 1.0 and original:
+        def pair(turns):                                         # the pair that turns so many times within `original`
+            return rot_dim * math.log(original / (turns * 2 * math.pi)) / (2 * math.log(base))
+        lo, hi = max(math.floor(pair(fast)), 0), min(math.ceil(pair(slow)), rot_dim - 1)
+        part = ((j - lo) / max(hi - lo, 1e-3)).clamp(0, 1)
+        freq = freq * (1 - part) + freq / factor * part
+        scale = 1.0 + 0.1 * math.log(factor)
+    else:
+        freq = freq / factor
+    return freq.to(device or torch.device("cuda", torch.cuda.current_device())), scale
 
 
 def sd_free(store: int) -> None:

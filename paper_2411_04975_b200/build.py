@@ -5,12 +5,14 @@ import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libsuffixspec.so")
-SOURCES = ["build.cu", "append.cu", "speculate.cu", "query.cu", "device_memory.cpp"]
+SOURCES = ["build.cu", "append.cu", "speculate.cu", "query.cu", "verify.cu", "attend.cu", "device_memory.cpp"]
 
 
 def call_path() -> str:
@@ -36,12 +38,15 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not fresh(LIB):
         nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
         cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-               "-shared", "-Xcompiler", "-fPIC", "-I", os.path.join(_ROOT, "include"), "-I", CSRC,
-               "-cudart", "shared", "-Xlinker", "-z", "-Xlinker", "nodelete", "-o", LIB]   # (a thread of device_memory.cpp outlives dlclose)
+               "-Xcompiler", "-fPIC", "-I", os.path.join(_ROOT, "include"), "-I", CSRC]
         if verbose:
             cmd += ["-Xptxas", "-v"]
-        cmd += [os.path.join(CSRC, f) for f in SOURCES]
-        subprocess.check_call(cmd)
+        with tempfile.TemporaryDirectory() as tmp:               # a compiler per file, side by side
+            objects = [os.path.join(tmp, f + ".o") for f in SOURCES]
+            with ThreadPoolExecutor(len(SOURCES)) as pool:
+                list(pool.map(lambda f, o: subprocess.check_call(cmd + ["-c", os.path.join(CSRC, f), "-o", o]), SOURCES, objects))
+            subprocess.check_call([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-Xcompiler", "-fPIC", "-cudart", "shared", "-Xlinker", "-z",
+                                   "-Xlinker", "nodelete", "-o", LIB, *objects])   # (a thread of device_memory.cpp outlives dlclose)
     if not fresh(call_path()):
         build_call()
     return LIB

@@ -1,0 +1,105 @@
+"""What the verifier's entry points refuse before any device is asked, and what the sizes of a call ask for."""
+import ctypes as C
+
+import pytest
+
+import paper_2411_04975_b200 as sfx
+from paper_2411_04975_b200 import binding
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return sfx.library()
+
+
+def cache(**kw):
+    c = dict(d_k=4096, d_v=8192, dtype=1, kv_heads=2, head_dim=64, n_layers=1, n_pages=4, page_size=16) | kw
+    line = c["kv_heads"] * c["head_dim"]
+    st = kw.get("strides", (0, c["page_size"] * line, line, c["head_dim"]))
+    c.pop("strides", None)
+    return binding._Cache(*c.values(), (C.c_int64 * 4)(*st), (C.c_int64 * 4)(*st))
+
+
+def rows(**kw):
+    r = dict(n=2, rows=10, max_draft=8, table_stride=2, d_offsets=256, d_cached=512, d_table=1024, d_mask=None, d_status=None) | kw
+    return binding._Rows(*r.values())
+
+
+def attend(lib, c, r, work=4096, size=1 << 40, **kw):
+    p = dict(q_heads=4, scale=1.0, window=0, sinks=0, shared=0) | {k: v for k, v in kw.items() if k in ("q_heads", "scale", "window", "sinks", "shared")}
+    prm = binding._AttendParams(*p.values(), (C.c_int64 * 2)(*kw.get("q_stride", (256, 64))), (C.c_int64 * 2)(*kw.get("out_stride", (256, 64))))
+    return lib.sd_attend(C.byref(c), C.byref(r), C.byref(prm), kw.get("q", 65536), kw.get("out", 131072), None, work, size, None)
+
+
+BAD_CACHES = [dict(dtype=3), dict(dtype=0), dict(head_dim=96), dict(head_dim=32), dict(kv_heads=0), dict(n_pages=0), dict(page_size=0), dict(page_size=12),
+              dict(page_size=4), dict(page_size=136), dict(d_k=None), dict(d_v=4104), dict(strides=(0, 2048, 130, 64)), dict(strides=(0, 2048, -128, 64)),
+              dict(strides=(0, 2048, 0, 64)), dict(n_layers=2, strides=(12, 2048, 128, 64)), dict(n_layers=0)]
+BAD_ROWS = [dict(n=-1), dict(rows=-1), dict(max_draft=65), dict(max_draft=-1), dict(table_stride=0), dict(table_stride=1 << 30), dict(d_cached=None), dict(d_table=None),
+            dict(d_offsets=None)]
+BAD_ATTEND = [dict(q_heads=3), dict(q_heads=0), dict(window=-1), dict(sinks=-2), dict(shared=-1), dict(scale=float("nan")), dict(q=65544), dict(q=None), dict(out=None),
+              dict(out=131080), dict(q_stride=(260, 64)), dict(out_stride=(256, 4)), dict(work=None), dict(work=4224)]
+
+
+@pytest.mark.parametrize("bad", BAD_CACHES + BAD_ROWS + BAD_ATTEND, ids=str)
+def test_attend_refuses(lib, bad):
+    c = cache(**bad) if bad in BAD_CACHES else cache()
+    r = rows(**bad) if bad in BAD_ROWS else rows()
+    assert attend(lib, c, r, **(bad if bad in BAD_ATTEND else {})) == -1
+
+
+def test_attend_refuses_null_structs(lib):
+    assert lib.sd_attend(None, None, None, None, None, None, None, 0, None) == -1
+    assert lib.sd_attend_workspace(None, None, None) == -1
+
+
+@pytest.mark.parametrize("bad", BAD_CACHES + BAD_ROWS, ids=str)
+def test_rotate_refuses(lib, bad):
+    c = cache(**bad) if bad in BAD_CACHES else cache()
+    r = rows(**bad) if bad in BAD_ROWS else rows()
+    two = [(C.c_int64 * 2)(256, 64) for _ in range(4)]
+    prm = binding._RotateParams(4, 64, 0, 1.0, 1e-6, *two)
+    assert lib.sd_rotate(C.byref(c), C.byref(r), C.byref(prm), 65536, 65536, 65536, 4096, None, None, None, 65536, None) == -1
+
+
+@pytest.mark.parametrize("bad", [dict(rot_dim=8), dict(rot_dim=-16), dict(rot_dim=80), dict(q_heads=5), dict(eps=-1.0), dict(eps=float("nan")), dict(freq=None), dict(q=65544),
+                                 dict(weight=4100), dict(stride=(256, 60))], ids=str)
+def test_rotate_refuses_its_own(lib, bad):
+    c, r = cache(), rows()
+    two = [(C.c_int64 * 2)(*bad.get("stride", (256, 64))) for _ in range(4)]
+    prm = binding._RotateParams(bad.get("q_heads", 4), bad.get("rot_dim", 64), 0, 1.0, bad.get("eps", 1e-6), *two)
+    assert lib.sd_rotate(C.byref(c), C.byref(r), C.byref(prm), bad.get("q", 65536), 65536, 65536, bad.get("freq", 4096), None, bad.get("weight"), None, 65536, None) == -1
+
+
+@pytest.mark.parametrize("bad", [dict(n=-1), dict(rows=-1), dict(M=65), dict(M=-1), dict(V=0), dict(V=(1 << 30) + 1), dict(dtype=0), dict(dtype=4), dict(stride=99), dict(logits=None),
+                                 dict(logits=4097), dict(path=None)], ids=str)
+def test_accept_refuses(lib, bad):
+    a = dict(n=2, rows=4, M=3, V=100, dtype=1, stride=100, logits=4096, offsets=256, tokens=256, parents=256, targets=256, path=256, begins=256, new=256, status=None) | bad
+    assert lib.sd_accept(*a.values(), None) == -1
+
+
+def test_commit_refuses(lib):
+    for bad in BAD_CACHES:
+        c, r = cache(**bad), rows()
+        assert lib.sd_commit(C.byref(c), C.byref(r), 4096, 4096, None) == -1, bad
+    c, r = cache(), rows()
+    assert lib.sd_commit(C.byref(c), C.byref(r), None, 4096, None) == -1
+    assert lib.sd_commit(C.byref(c), C.byref(r), 4096, None, None) == -1
+
+
+def test_tensors_that_are_no_device_memory_are_refused():
+    import torch
+    q = torch.zeros(3, 4, 64, dtype=torch.bfloat16)
+    k = torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16)
+    i = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(TypeError, match="k_cache: expected a tensor on the current CUDA device"):
+        binding._PlainCall(sfx.library()).attend(q, k, k, i[None], i, i, None, 1.0, 0, 0, 0, q, None, None)
+
+
+def test_plain_calls_take_the_same_arguments():
+    import inspect
+    sfx.library()
+    native = binding._load_call(binding._lib)
+    for name in ("rotate", "attend", "accept", "commit"):
+        n = len(inspect.signature(getattr(binding._PlainCall(binding._lib), name)).parameters)
+        with pytest.raises(TypeError, match=f"{n} arguments expected"):
+            getattr(native, name)()
