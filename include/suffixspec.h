@@ -58,7 +58,9 @@ enum {
                                   /* growing at the last good token                   */
     SD_STATUS_BAD_ROWS = 16,      /* sd_rotate ... sd_commit: the request's rows, its */
                                   /* length or its path make no sense; left out       */
-    SD_STATUS_BAD_PAGE = 32       /* a page outside the cache was met                 */
+    SD_STATUS_BAD_PAGE = 32,      /* a page outside the cache was met                 */
+    SD_STATUS_FAILED = 64         /* sd_attend gave up waiting on the device: nothing */
+                                  /* of the call is of use                            */
 };
 
 /* sd_spec_params.flags */
