@@ -1,13 +1,19 @@
 // The verifier's side of a step beside attention: sd_rotate, sd_accept, sd_commit.
 #include "verify.cuh"
 
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
 namespace {
 
 // ---- sd_rotate -----------------------------------------------------------------------------
-// A block per row; the row's heads go to groups of head_dim / 8 lanes, eight elements a lane.  Bound by the bytes of
-// the row: every element is read once and written once.
+// A block takes a few rows of one request (one, where there are few; ROT_ROWS in a large batch), so that what it looks up - where the rows are, how deep,
+// in which page - is two reads behind one another for all of them.  The rows' heads go to groups of head_dim / 8 lanes, eight
+// elements a lane.  Bound by the bytes of the rows: every element is read once and written once.
 constexpr int ROT_THREADS = 256;
-constexpr int ROT_BATCH = 4;                                      // heads of a group that are loaded before any is worked on
+constexpr int ROT_ROWS = 4;
+constexpr int ROT_BATCH = 6;                                      // pieces that a lane has under way
 
 struct RotateArgs {
     sd_cache c;
@@ -17,87 +23,84 @@ struct RotateArgs {
     const double* freq;
     const int32_t* positions;
     void* out;
+    int chunks, per;              // of a request: blocks, rows a block
 };
 
 template <class T, int D, bool INTERLEAVED>
 __global__ void __launch_bounds__(ROT_THREADS) rotate_kernel(const __grid_constant__ RotateArgs a) {
     sd_chain_begin();
     constexpr int LANES = D / 8, GROUPS = ROT_THREADS / LANES;
-    __shared__ float s_cos[D / 2], s_sin[D / 2];
-    __shared__ int s_line;                                        // of the page; -1: rows and page make no sense
-    __shared__ int s_page;
+    __shared__ float2 s_turn[ROT_ROWS][D / 2];                    // cosine and sine
+    __shared__ long long s_k[ROT_ROWS], s_v[ROT_ROWS];            // the row's line in the caches; -1: in no page
     const int t = threadIdx.x, lane = t % LANES, group = t / LANES;
     const sd_rows& b = a.b;
+    const int i = blockIdx.x / a.chunks, first_row = blockIdx.x % a.chunks * a.per;
+    const Request r = sd_request(b, i, a.c.page_size);
+    if (b.d_status && first_row == 0 && t == ROT_THREADS - 1) {
+        int st = r.status;
+        if (r.count)
+            for (int e = r.cached / a.c.page_size; e <= (r.cached + r.count - 1) / a.c.page_size; ++e)
+                if (sd_page(b, a.c.n_pages, i, e) < 0) st |= SD_STATUS_BAD_PAGE;
+        b.d_status[i] = st;
+    }
+    const int rows = min(a.per, r.count - first_row);
+    if (rows <= 0) return;
+    const long long begin = r.begin + first_row;
+    const int q_heads = a.p.q_heads, k_end = q_heads + a.c.kv_heads, heads = k_end + a.c.kv_heads, pieces = rows * heads;
 
-    if (b.d_status && t == ROT_THREADS - 1)
-        for (int i = blockIdx.x; i < b.n; i += gridDim.x) {
-            const Request r = sd_request(b, i, a.c.page_size);
-            int st = r.status;
-            if (r.count)
-                for (int e = r.cached / a.c.page_size; e <= (r.cached + r.count - 1) / a.c.page_size; ++e)
-                    if (sd_page(b, a.c.n_pages, i, e) < 0) st |= SD_STATUS_BAD_PAGE;
-            b.d_status[i] = st;
-        }
-    const long long row = blockIdx.x;
-    if (row >= b.rows) return;
-    const int heads = a.p.q_heads + 2 * a.c.kv_heads;
-
-    auto source = [&](int h) -> const T* {
-        if (h < a.p.q_heads) return (const T*)a.q + row * a.p.q_stride[0] + h * a.p.q_stride[1];
-        h -= a.p.q_heads;
-        if (h < a.c.kv_heads) return (const T*)a.k + row * a.p.k_stride[0] + h * a.p.k_stride[1];
-        return (const T*)a.v + row * a.p.v_stride[0] + (h - a.c.kv_heads) * a.p.v_stride[1];
+    auto source = [&](int piece) -> const uint4* {
+        const int e = piece / heads, h = piece - e * heads;
+        const T* p = h < q_heads ? (const T*)a.q + (begin + e) * a.p.q_stride[0] + h * a.p.q_stride[1]
+                     : h < k_end ? (const T*)a.k + (begin + e) * a.p.k_stride[0] + (h - q_heads) * a.p.k_stride[1]
+                                 : (const T*)a.v + (begin + e) * a.p.v_stride[0] + (h - k_end) * a.p.v_stride[1];
+        return (const uint4*)p + lane;
     };
     uint4 raw[ROT_BATCH];
 #pragma unroll
     for (int e = 0; e < ROT_BATCH; ++e)
-        if (group + e * GROUPS < heads) raw[e] = *(const uint4*)(source(group + e * GROUPS) + lane * 8);
+        if (group + e * GROUPS < pieces) raw[e] = *source(group + e * GROUPS);
 
-    int i = 0;                                                    // the request: offsets that are not above the row
-    for (int base = 0; base < b.n; base += ROT_THREADS)
-        i += __syncthreads_count(base + t < b.n && b.d_offsets[base + t + 1] <= row);
-    if (i >= b.n) return;                                         // behind the last request
-    const Request r = sd_request(b, i, a.c.page_size);
-    if (row < r.begin || row >= r.begin + r.count) return;
-    const int local = (int)(row - r.begin);
-    if (t == 0) {
-        const int place = r.cached + local;
-        s_page = sd_page(b, a.c.n_pages, i, place / a.c.page_size);
-        s_line = place % a.c.page_size;
+    const int half = a.p.rot_dim / 2;
+    if (t < rows) {
+        const int place = r.cached + first_row + t, page = sd_page(b, a.c.n_pages, i, place / a.c.page_size), line = place % a.c.page_size;
+        s_k[t] = page < 0 ? -1 : page * a.c.k_stride[1] + line * a.c.k_stride[2];
+        s_v[t] = page < 0 ? -1 : page * a.c.v_stride[1] + line * a.c.v_stride[2];
     }
-    if (t < a.p.rot_dim / 2) {
-        const int pos = a.positions ? a.positions[row] : r.cached + __popcll(sd_tree_bits(b, i, local));
-        double turns = (double)pos * a.freq[t] * 0.15915494309189533577;      // 1 / 2 pi
+    for (int e = t; e < rows * (D / 2); e += ROT_THREADS) {
+        const int row = e / (D / 2), j = e % (D / 2);
+        if (j >= half) continue;
+        const int pos = a.positions ? a.positions[begin + row] : r.cached + __popcll(sd_tree_bits(b, i, first_row + row));
+        double turns = (double)pos * a.freq[j] * 0.15915494309189533577;      // 1 / 2 pi
         turns -= rint(turns);
         float sn, cs;
         sincospif(2.0f * (float)turns, &sn, &cs);
-        s_cos[t] = cs * a.p.scale;
-        s_sin[t] = sn * a.p.scale;
+        s_turn[row][j] = make_float2(cs * a.p.scale, sn * a.p.scale);
     }
     __syncthreads();
-    const int half = a.p.rot_dim / 2;
-    const long long in_k = s_page * a.c.k_stride[1] + s_line * a.c.k_stride[2], in_v = s_page * a.c.v_stride[1] + s_line * a.c.v_stride[2];
+    const int at = lane * 8;
+    const bool turned = at < a.p.rot_dim, low = at < half;
+    const int other = (t & 31 & ~(LANES - 1)) + (turned ? (low ? lane + half / 8 : lane - half / 8) : lane);
 
-    for (int base = 0; base < heads; base += GROUPS * ROT_BATCH) {
-        const int first = base + group;
+    for (int base = 0; base < pieces; base += GROUPS * ROT_BATCH) {
         if (base) {
 #pragma unroll
             for (int e = 0; e < ROT_BATCH; ++e)
-                if (first + e * GROUPS < heads) raw[e] = *(const uint4*)(source(first + e * GROUPS) + lane * 8);
+                if (base + group + e * GROUPS < pieces) raw[e] = *source(base + group + e * GROUPS);
         }
 #pragma unroll
         for (int e = 0; e < ROT_BATCH; ++e) {
-            const int h = first + e * GROUPS;
-            const bool live = h < heads;                          // (all lanes stay for the shuffles)
-            if (live && h >= a.p.q_heads + a.c.kv_heads) {
-                if (s_page >= 0)
-                    *(uint4*)((T*)a.c.d_v + in_v + (h - a.p.q_heads - a.c.kv_heads) * a.c.v_stride[3] + lane * 8) = raw[e];
+            const int piece = base + group + e * GROUPS;
+            if (base + e * GROUPS >= pieces) break;               // (the same for all: lanes stay together for the shuffles)
+            const bool live = piece < pieces;
+            const int row = live ? piece / heads : 0, h = live ? piece - row * heads : 0;
+            if (live && h >= k_end) {
+                if (s_v[row] >= 0) ((uint4*)((T*)a.c.d_v + s_v[row] + (h - k_end) * a.c.v_stride[3]))[lane] = raw[e];
             }
             float x[8], y[8];
             sd_unpack<T>(raw[e], x);
-            const bool is_q = h < a.p.q_heads;
-            const T* w = (const T*)(is_q ? a.qw : a.kw);
+            const bool is_q = h < q_heads;
             if (a.qw || a.kw) {
+                const T* w = (const T*)(is_q ? a.qw : a.kw);
                 float sum = 0.f;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) sum += x[k] * x[k];
@@ -106,38 +109,32 @@ __global__ void __launch_bounds__(ROT_THREADS) rotate_kernel(const __grid_consta
                 if (w) {
                     const float inv = 1.0f / sqrtf(sum / D + a.p.eps);
                     float wf[8];
-                    sd_unpack<T>(*(const uint4*)(w + lane * 8), wf);
+                    sd_unpack<T>(((const uint4*)w)[lane], wf);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) x[k] = x[k] * inv * wf[k];
                 }
             }
-            const int at = lane * 8;
             if (INTERLEAVED) {
 #pragma unroll
                 for (int k = 0; k < 8; k += 2) {
-                    y[k] = x[k]; y[k + 1] = x[k + 1];
-                    if (at < a.p.rot_dim) {
-                        const float c = s_cos[(at + k) / 2], s = s_sin[(at + k) / 2];
-                        y[k] = x[k] * c - x[k + 1] * s;
-                        y[k + 1] = x[k + 1] * c + x[k] * s;
-                    }
+                    const float2 c = turned ? s_turn[row][(at + k) / 2] : make_float2(1.f, 0.f);
+                    y[k] = turned ? x[k] * c.x - x[k + 1] * c.y : x[k];
+                    y[k + 1] = turned ? x[k + 1] * c.x + x[k] * c.y : x[k + 1];
                 }
             } else {
-                const bool low = at < half;
-                const int other = (threadIdx.x & 31 & ~(LANES - 1)) + (at < a.p.rot_dim ? (low ? lane + half / 8 : lane - half / 8) : lane);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const float z = __shfl_sync(~0u, x[k], other);
                     y[k] = x[k];
-                    if (at < a.p.rot_dim) {
-                        const int j = low ? at + k : at + k - half;
-                        y[k] = low ? x[k] * s_cos[j] - z * s_sin[j] : x[k] * s_cos[j] + z * s_sin[j];
+                    if (turned) {
+                        const float2 c = s_turn[row][low ? at + k : at + k - half];
+                        y[k] = low ? x[k] * c.x - z * c.y : x[k] * c.x + z * c.y;
                     }
                 }
             }
-            if (!live || h >= a.p.q_heads + a.c.kv_heads) continue;
-            if (is_q) *(uint4*)((T*)a.out + row * a.p.out_stride[0] + h * a.p.out_stride[1] + at) = sd_pack<T>(y);
-            else if (s_page >= 0) *(uint4*)((T*)a.c.d_k + in_k + (h - a.p.q_heads) * a.c.k_stride[3] + at) = sd_pack<T>(y);
+            if (!live || h >= k_end) continue;
+            if (is_q) ((uint4*)((T*)a.out + (begin + row) * a.p.out_stride[0] + h * a.p.out_stride[1]))[lane] = sd_pack<T>(y);
+            else if (s_k[row] >= 0) ((uint4*)((T*)a.c.d_k + s_k[row] + (h - q_heads) * a.c.k_stride[3]))[lane] = sd_pack<T>(y);
         }
     }
 }
@@ -160,46 +157,81 @@ __device__ __forceinline__ uint32_t order_key(float f) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// The largest of a chunk of 16 bytes.
+__device__ __forceinline__ uint32_t largest(const uint4& v, float) {
+    return max(max(order_key(__uint_as_float(v.x)), order_key(__uint_as_float(v.y))), max(order_key(__uint_as_float(v.z)), order_key(__uint_as_float(v.w))));
+}
+__device__ __forceinline__ uint32_t largest(const uint4& v, __nv_bfloat16) {
+    __nv_bfloat162 h[4];
+    memcpy(h, &v, 16);
+    const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+    return max(order_key(__low2float(m)), order_key(__high2float(m)));
+}
+__device__ __forceinline__ uint32_t largest(const uint4& v, __half) {
+    __half2 h[4];
+    memcpy(h, &v, 16);
+    const __half2 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+    return max(order_key(__low2float(m)), order_key(__high2float(m)));
+}
+
+// A cluster of `blocks` blocks a row; the first gets the others' results and says what it is.
 template <class T>
-__global__ void __launch_bounds__(MAX_THREADS) row_max_kernel(const T* logits, long long stride, int vocab, int32_t* targets) {
+__global__ void __launch_bounds__(MAX_THREADS) row_max_kernel(const T* logits, long long stride, int vocab, int32_t* targets, int blocks) {
     sd_chain_begin();
-    constexpr int PER = 16 / sizeof(T);
-    const T* row = logits + blockIdx.x * stride;
+    constexpr int PER = 16 / sizeof(T), AHEAD = 4;
+    const int rank = blockIdx.x % blocks, first = rank * MAX_THREADS, step = blocks * MAX_THREADS;
+    const long long r = blockIdx.x / blocks;
+    const T* row = logits + r * stride;
     const int t = threadIdx.x;
     const int head = min(vocab, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T));   // elements before the first 16-byte boundary
-    const int chunks = 1 + (vocab - head + PER - 1) / PER;
-    auto bounds = [&](int c, int& lo, int& hi) {
-        lo = c == 0 ? 0 : head + (c - 1) * PER;
-        hi = c == 0 ? head : min(lo + PER, vocab);
-    };
+    const int whole = (vocab - head) / PER, tail = head + whole * PER;
+    const uint4* chunk = (const uint4*)(row + head);
     uint32_t best = 0;
-    int where = 0;
-    for (int c = t; c < chunks; c += MAX_THREADS) {
-        int lo, hi;
-        bounds(c, lo, hi);
-        uint32_t m = 0;
-        if (hi - lo == PER && c > 0) {
-            T v[PER];
-            *(uint4*)v = *(const uint4*)(row + lo);
+    int where = 0;                                                // chunk; -1: what is before them, `whole`: what is behind
+    if (rank == 0 && t < head) { best = order_key(as_float(row[t])); where = -1; }
+    int c = first + t;
+    for (; c + (AHEAD - 1) * step < whole; c += AHEAD * step) {
+        uint4 v[AHEAD];
 #pragma unroll
-            for (int k = 0; k < PER; ++k) m = max(m, order_key(as_float(v[k])));
-        } else {
-            for (int k = lo; k < hi; ++k) m = max(m, order_key(as_float(row[k])));
+        for (int e = 0; e < AHEAD; ++e) v[e] = __ldcs(chunk + c + e * step);
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) {
+            const uint32_t m = largest(v[e], T());
+            if (m > best) { best = m; where = c + e * step; }
         }
+    }
+    for (; c < whole; c += step) {
+        const uint32_t m = largest(__ldcs(chunk + c), T());
         if (m > best) { best = m; where = c; }
     }
-    unsigned long long all = (unsigned long long)best << 32 | (0xFFFFFFFFu - (uint32_t)where);
+    if (rank == 0 && t < vocab - tail) {
+        const uint32_t m = order_key(as_float(row[tail + t]));
+        if (m > best) { best = m; where = whole; }
+    }
+    unsigned long long all = (unsigned long long)best << 32 | (0xFFFFFFFEu - (uint32_t)where);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) all = max(all, __shfl_xor_sync(~0u, all, d));
-    __shared__ unsigned long long s_all[MAX_THREADS / 32];
+    __shared__ unsigned long long s_all[MAX_THREADS / 32], s_block[8];
     if ((t & 31) == 0) s_all[t / 32] = all;
     __syncthreads();
-    if (t == 0) {
-        for (int w = 1; w < MAX_THREADS / 32; ++w) all = max(all, s_all[w]);
-        int lo, hi;
-        bounds((int)(0xFFFFFFFFu - (uint32_t)all), lo, hi);
-        for (int k = lo; k < hi; ++k)
-            if (order_key(as_float(row[k])) == (uint32_t)(all >> 32)) { targets[blockIdx.x] = k; break; }
+    if (t < 32) {
+        all = t < MAX_THREADS / 32 ? s_all[t] : 0;
+#pragma unroll
+        for (int d = MAX_THREADS / 64; d > 0; d >>= 1) all = max(all, __shfl_xor_sync(~0u, all, d));
+    }
+    if (blocks > 1) {
+        auto cluster = cooperative_groups::this_cluster();
+        if (t == 0) *cluster.map_shared_rank(&s_block[rank], 0) = all;
+        cluster.sync();
+        if (rank) return;
+        all = 0;
+        for (int e = 0; e < blocks; ++e) all = max(all, s_block[e]);
+    }
+    if (t < 32) {
+        const int won = (int)(0xFFFFFFFEu - (uint32_t)all), lo = won < 0 ? 0 : head + won * PER, n = won < 0 ? head : min(PER, vocab - lo);
+        const bool it = t < n && order_key(as_float(row[lo + t])) == (uint32_t)(all >> 32);
+        const unsigned found = __ballot_sync(~0u, it);
+        if (t == 0) targets[r] = lo + __ffs(found) - 1;
     }
 }
 
@@ -212,13 +244,17 @@ struct WalkArgs {
     int32_t *new_tokens, *status;
 };
 
-// The accepted paths, a warp each, then their begins and tokens, by one block.
-__global__ void __launch_bounds__(1024) walk_kernel(const WalkArgs a) {
+// The accepted paths, a warp each, then their begins and tokens.  One block, or a cluster of them that take a part of the requests each and tell the others how
+// many tokens it has.
+constexpr int WALK_THREADS = 512, WALK_BLOCKS = 8;
+
+__global__ void __launch_bounds__(WALK_THREADS) walk_kernel(const WalkArgs a) {
     sd_chain_begin();
-    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    __shared__ long long s_sum[32];
-    __shared__ long long s_base;
-    for (int i = warp; i < a.n; i += 32) {
+    constexpr int WARPS = WALK_THREADS / 32;
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5, blocks = gridDim.x, rank = blockIdx.x;
+    __shared__ long long s_sum[WARPS], s_base, s_block[WALK_BLOCKS];
+    const int part = (a.n + blocks - 1) / blocks, lo_i = min(rank * part, a.n), hi_i = min(lo_i + part, a.n);
+    for (int i = lo_i + warp; i < hi_i; i += WARPS) {
         const long long lo = a.offsets[i], hi = a.offsets[i + 1];
         const bool bad = lo < 0 || hi < lo || hi > a.rows || hi - lo > a.M + 1;
         const int count = bad ? 0 : (int)(hi - lo);
@@ -252,10 +288,31 @@ __global__ void __launch_bounds__(1024) walk_kernel(const WalkArgs a) {
             if (a.status) a.status[i] = bad ? SD_STATUS_BAD_ROWS : SD_STATUS_OK;
         }
     }
-    if (t == 0) { a.new_offsets[0] = 0; s_base = 0; }
     __syncthreads();
-    for (int first = 0; first < a.n; first += 1024) {             // begins: running sums of the lengths
-        long long x = first + t < a.n ? a.new_offsets[first + t + 1] : 0;
+    long long mine = 0;                                           // tokens of the block's requests
+    if (blocks > 1) {
+        for (int i = lo_i + t; i < hi_i; i += WALK_THREADS) mine += a.new_offsets[i + 1];
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(~0u, mine, d);
+        if (lane == 0) s_sum[warp] = mine;
+        __syncthreads();
+        auto cluster = cooperative_groups::this_cluster();
+        if (t < blocks) {
+            mine = 0;
+            for (int w = 0; w < WARPS; ++w) mine += s_sum[w];
+            *cluster.map_shared_rank(&s_block[rank], t) = mine;
+        }
+        cluster.sync();
+    }
+    if (t == 0) {
+        long long before = 0;
+        for (int e = 0; e < rank; ++e) before += s_block[e];
+        s_base = before;
+        if (rank == 0) a.new_offsets[0] = 0;
+    }
+    __syncthreads();
+    for (int first = lo_i; first < hi_i; first += WALK_THREADS) {  // begins: running sums of the lengths
+        long long x = first + t < hi_i ? a.new_offsets[first + t + 1] : 0;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const long long y = __shfl_up_sync(~0u, x, d);
@@ -263,116 +320,100 @@ __global__ void __launch_bounds__(1024) walk_kernel(const WalkArgs a) {
         }
         if (lane == 31) s_sum[warp] = x;
         __syncthreads();
-        if (warp == 0) {
-            long long y = s_sum[lane];
+        x += s_base;
+        for (int w = 0; w < warp; ++w) x += s_sum[w];
+        if (first + t < hi_i) a.new_offsets[first + t + 1] = x;
+        __syncthreads();
+        if (t == WALK_THREADS - 1) s_base = x;
+        __syncthreads();
+    }
+    for (int i = lo_i + warp; i < hi_i; i += WARPS) {
+        const long long lo = a.offsets[i], end = a.new_offsets[i + 1];
+        const int32_t* path = a.path + (long long)i * (a.M + 1);
+        int p[3], kept = 0;
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const long long z = __shfl_up_sync(~0u, y, d);
-                if (lane >= d) y += z;
-            }
-            s_sum[lane] = y;
+        for (int e = 0; e < 3; ++e) {
+            p[e] = lane + 32 * e <= a.M ? path[lane + 32 * e] : -1;
+            kept += __popc(__ballot_sync(~0u, p[e] >= 0));
         }
-        __syncthreads();
-        x += s_base + (warp ? s_sum[warp - 1] : 0);
-        if (first + t < a.n) a.new_offsets[first + t + 1] = x;
-        __syncthreads();
-        if (t == 1023) s_base = x;
-        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (p[e] >= 0) a.new_tokens[end - kept + lane + 32 * e] = a.targets[lo + p[e]];
     }
-    for (int i = warp; i < a.n; i += 32) {
-        const long long lo = a.offsets[i], at = a.new_offsets[i];
-        const int kept = (int)(a.new_offsets[i + 1] - at);
-        for (int j = lane; j < kept; j += 32) a.new_tokens[at + j] = a.targets[lo + a.path[(long long)i * (a.M + 1) + j]];
-    }
-    for (long long k = s_base + t; k < a.rows; k += 1024) a.new_tokens[k] = -1;
+    if (rank == blocks - 1)
+        for (long long k = s_base + t; k < a.rows; k += WALK_THREADS) a.new_tokens[k] = -1;
 }
 
 // ---- sd_commit -----------------------------------------------------------------------------
-// A block per request, layer and one of keys and values; a thread per 16 bytes of a line.  Lines only move to smaller places, and a
-// path ascends: what a batch of lines overwrites, no later batch reads.  Bound by the lines moved (and by the latency of path, table, line).
-constexpr int COMMIT_BATCH = 8;
+// A cluster per request, whose blocks take the planes (keys or values of a layer) in turns; a thread per 16 bytes of a line.  Lines only move to smaller
+// places, and a path ascends: what a batch of lines overwrites, no later batch reads.  The new length is written when all blocks have read the old one, which
+// may be the same memory.  Bound by the lines moved (and by the latency of path, table, line).
+constexpr int COMMIT_BATCH = 4, COMMIT_THREADS = 256;
 
 struct CommitArgs {
     sd_cache c;
     sd_rows b;
     const int32_t* path;
     int32_t* cached_out;
+    int blocks;
 };
 
-__global__ void __launch_bounds__(128) commit_kernel(const __grid_constant__ CommitArgs a) {
+__global__ void __launch_bounds__(COMMIT_THREADS) commit_kernel(const __grid_constant__ CommitArgs a) {
     sd_chain_begin();
     const sd_rows& b = a.b;
-    const int i = blockIdx.x, side = blockIdx.y & 1, layer = blockIdx.y >> 1, t = threadIdx.x;
-    __shared__ int s_path[SD_MAX_SPEC + 1], s_src[SD_MAX_SPEC + 1], s_dst[SD_MAX_SPEC + 1];     // pages
-    __shared__ int s_bad;
-    const int M1 = b.max_draft + 1;
-    if (t == 0) s_bad = 0;
-    __syncthreads();
+    const int i = blockIdx.x / a.blocks, rank = blockIdx.x % a.blocks, t = threadIdx.x;
+    __shared__ long long s_src[2][SD_MAX_SPEC + 1], s_dst[2][SD_MAX_SPEC + 1];      // of keys, of values: elements from the plane's begin
+    __shared__ int s_moves, s_bad;
+    const int M1 = b.max_draft + 1, P = a.c.page_size;
+    if (t == 0) { s_bad = 0; s_moves = 0; }
     const int cached = b.d_cached[i];
-    int p = -1, kept;
-    const int P = a.c.page_size;
-    if (t < M1) p = a.path[(long long)i * M1 + t];
-    kept = __syncthreads_count(p >= 0);
-    if (t < M1) {
-        s_path[t] = p;
-        const int before = t ? a.path[(long long)i * M1 + t - 1] : -1;
-        bool bad = t < kept ? p <= before || p > b.max_draft || (t == 0 && p != 0) : p != -1;
-        if (t < kept && !bad) {
-            if (cached < 0 || (long long)cached + p >= (long long)P * b.table_stride) bad = true;
-            else {
-                s_src[t] = sd_page(b, a.c.n_pages, i, (cached + p) / P);
-                s_dst[t] = sd_page(b, a.c.n_pages, i, (cached + t) / P);
-                if (p != t && (s_src[t] < 0 || s_dst[t] < 0)) atomicOr(&s_bad, SD_STATUS_BAD_PAGE);
-            }
+    const int32_t* path = a.path + (long long)i * M1;
+    const int p = t < M1 ? path[t] : -1, before = t > 0 && t < M1 ? path[t - 1] : -1;
+    const int kept = __syncthreads_count(p >= 0);
+    if (t < M1 && (t < kept ? p <= before || p > b.max_draft || (t == 0 && p != 0) || cached < 0 || (long long)cached + p >= (long long)P * b.table_stride : p != -1))
+        atomicOr(&s_bad, SD_STATUS_BAD_ROWS);
+    const int bad_rows = __syncthreads_or(s_bad);
+    if (!bad_rows) {                                              // (behind the first row that moves all do)
+        const bool moves = t < kept && p != t;
+        int src = -1, dst = -1;
+        if (moves) {
+            src = sd_page(b, a.c.n_pages, i, (cached + p) / P);
+            dst = sd_page(b, a.c.n_pages, i, (cached + t) / P);
+            if (src < 0 || dst < 0) atomicOr(&s_bad, SD_STATUS_BAD_PAGE);
         }
-        if (bad) atomicOr(&s_bad, SD_STATUS_BAD_ROWS);
+        if (moves) {
+            const bool lines = src >= 0 && dst >= 0;
+            const int sl = (cached + p) % P, dl = (cached + t) % P;
+            s_src[0][t] = lines ? src * a.c.k_stride[1] + sl * a.c.k_stride[2] : -1;
+            s_dst[0][t] = dst * a.c.k_stride[1] + dl * a.c.k_stride[2];
+            s_src[1][t] = src * a.c.v_stride[1] + sl * a.c.v_stride[2];
+            s_dst[1][t] = dst * a.c.v_stride[1] + dl * a.c.v_stride[2];
+            atomicAdd(&s_moves, 1);
+        }
     }
     __syncthreads();
-    const int bad = s_bad;
-    if (blockIdx.y == 0 && t == 0) {
-        if (b.d_status) b.d_status[i] = bad;
-    }
-    (void)layer; (void)side;
-    if (!(bad & SD_STATUS_BAD_ROWS)) {
-        const int64_t* st = side ? a.c.v_stride : a.c.k_stride;
-        char* base = (char*)(side ? a.c.d_v : a.c.d_k) + 2 * (layer * st[0]);
-        const int per = a.c.head_dim / 8, columns = a.c.kv_heads * per;
-        for (int col = t; col < columns; col += blockDim.x) {
-            char* at = base + 2 * ((col / per) * st[3] + (col % per) * 8);
-            for (int first = 0; first < kept; first += COMMIT_BATCH) {
+    if (!bad_rows && s_moves) {
+        const int begin = kept - s_moves, per = a.c.head_dim / 8, columns = a.c.kv_heads * per;
+        for (int e = rank * COMMIT_THREADS + t; e < 2 * a.c.n_layers * columns; e += a.blocks * COMMIT_THREADS) {
+            const int plane = e / columns, col = e - plane * columns, side = plane & 1, head = col / per;
+            const int64_t* st = side ? a.c.v_stride : a.c.k_stride;
+            uint16_t* at = (uint16_t*)(side ? a.c.d_v : a.c.d_k) + (plane >> 1) * st[0] + head * st[3] + (col - head * per) * 8;
+            for (int first = begin; first < kept; first += COMMIT_BATCH) {
                 uint4 v[COMMIT_BATCH];
 #pragma unroll
-                for (int e = 0; e < COMMIT_BATCH; ++e) {
-                    const int j = first + e;
-                    if (j < kept && s_path[j] != j && s_src[j] >= 0 && s_dst[j] >= 0)
-                        v[e] = *(const uint4*)(at + 2 * (s_src[j] * st[1] + (cached + s_path[j]) % P * st[2]));
-                }
+                for (int j = 0; j < COMMIT_BATCH; ++j)
+                    if (first + j < kept && s_src[0][first + j] >= 0) v[j] = *(const uint4*)(at + s_src[side][first + j]);
 #pragma unroll
-                for (int e = 0; e < COMMIT_BATCH; ++e) {
-                    const int j = first + e;
-                    if (j < kept && s_path[j] != j && s_src[j] >= 0 && s_dst[j] >= 0)
-                        *(uint4*)(at + 2 * (s_dst[j] * st[1] + (cached + j) % P * st[2])) = v[e];
-                }
+                for (int j = 0; j < COMMIT_BATCH; ++j)
+                    if (first + j < kept && s_src[0][first + j] >= 0) *(uint4*)(at + s_dst[side][first + j]) = v[j];
             }
         }
     }
-}
-
-// After the lines: the new lengths (the other kernel's blocks read the old ones, which may be the same memory).
-__global__ void __launch_bounds__(128) lengths_kernel(const __grid_constant__ CommitArgs a) {
-    sd_chain_begin();
-    const int i = blockIdx.x * 128 + threadIdx.x;
-    if (i >= a.b.n) return;
-    const int M1 = a.b.max_draft + 1, cached = a.b.d_cached[i];
-    int kept = 0, before = -1;
-    bool bad = false;
-    for (int j = 0; j < M1; ++j) {
-        const int p = a.path[(long long)i * M1 + j];
-        if (p >= 0) bad |= kept != j || p <= before || p > a.b.max_draft || (j == 0 && p != 0) || (long long)cached + p >= (long long)a.c.page_size * a.b.table_stride;
-        else bad |= p != -1;
-        if (p >= 0) { ++kept; before = p; }
+    if (a.blocks > 1) cooperative_groups::this_cluster().sync();
+    if (rank == 0 && t == 0) {
+        a.cached_out[i] = bad_rows ? cached : cached + kept;
+        if (b.d_status) b.d_status[i] = s_bad;
     }
-    a.cached_out[i] = bad || (kept && cached < 0) ? cached : cached + kept;
 }
 
 }  // namespace
@@ -397,8 +438,11 @@ extern "C" int sd_rotate(const sd_cache* cache, const sd_rows* rows, const sd_ro
     }
     rc = sd_check_pointer(cache->d_k);
     if (rc != SD_OK) return rc;
-    const RotateArgs a = {*cache, *rows, *prm, d_q, d_k, d_v, d_q_weight, d_k_weight, d_freq, d_positions, d_q_out};
-    const unsigned grid = rows->rows > 0 ? rows->rows : 1;
+    // A row a block while that makes no more blocks than are at work at once; else four, which look up together.
+    const int most = rows->max_draft + 1, per = (long long)rows->n * most <= 1024 ? 1 : ROT_ROWS, chunks = (std::min(most, std::max(rows->rows, 1)) + per - 1) / per;
+    if ((long long)rows->n * chunks > 0x7FFFFFFF) return SD_ERR_INVALID_ARG;
+    const RotateArgs a = {*cache, *rows, *prm, d_q, d_k, d_v, d_q_weight, d_k_weight, d_freq, d_positions, d_q_out, chunks, per};
+    const unsigned grid = rows->n * chunks;
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e;
 #define SD_ROTATE(T, D) (prm->interleaved ? sd_launch(rotate_kernel<T, D, true>, grid, ROT_THREADS, 0, st, a) : sd_launch(rotate_kernel<T, D, false>, grid, ROT_THREADS, 0, st, a))
@@ -420,14 +464,18 @@ extern "C" int sd_accept(int32_t n, int32_t rows, int32_t max_draft, int32_t voc
     if (rc != SD_OK) return rc;
     cudaStream_t st = (cudaStream_t)stream;
     if (rows > 0) {
+        // Up to eight blocks a row where the rows are too few to fill the device.
+        int blocks = 1;
+        while (blocks < 8 && rows * blocks < 128 && vocab / blocks >= 16 * MAX_THREADS) blocks *= 2;
         cudaError_t e;
-        if (dtype == SD_BF16) e = sd_launch(row_max_kernel<__nv_bfloat16>, rows, MAX_THREADS, 0, st, (const __nv_bfloat16*)d_logits, (long long)row_stride, vocab, d_targets);
-        else if (dtype == SD_FP16) e = sd_launch(row_max_kernel<__half>, rows, MAX_THREADS, 0, st, (const __half*)d_logits, (long long)row_stride, vocab, d_targets);
-        else e = sd_launch(row_max_kernel<float>, rows, MAX_THREADS, 0, st, (const float*)d_logits, (long long)row_stride, vocab, d_targets);
+#define SD_ROW_MAX(T) sd_launch_clusters(row_max_kernel<T>, (unsigned)rows * blocks, blocks, MAX_THREADS, 0, st, (const T*)d_logits, (long long)row_stride, vocab, d_targets, blocks)
+        e = dtype == SD_BF16 ? SD_ROW_MAX(__nv_bfloat16) : dtype == SD_FP16 ? SD_ROW_MAX(__half) : SD_ROW_MAX(float);
+#undef SD_ROW_MAX
         if (e != cudaSuccess) return SD_ERR_CUDA;
     }
     const WalkArgs a = {n, rows, max_draft, d_offsets, d_tokens, d_parents, d_targets, d_path, d_new_offsets, d_new_tokens, d_status};
-    return sd_launch(walk_kernel, 1, 1024, 0, st, a) == cudaSuccess ? SD_OK : SD_ERR_CUDA;
+    const int blocks = n > WALK_THREADS / 32 ? WALK_BLOCKS : 1;   // (a warp a request)
+    return sd_launch_clusters(walk_kernel, blocks, blocks, WALK_THREADS, 0, st, a) == cudaSuccess ? SD_OK : SD_ERR_CUDA;
 }
 
 extern "C" int sd_commit(const sd_cache* cache, const sd_rows* rows, const int32_t* d_path, int32_t* d_new_cached, void* stream) {
@@ -438,14 +486,12 @@ extern "C" int sd_commit(const sd_cache* cache, const sd_rows* rows, const int32
     if (!d_path || !d_new_cached) return SD_ERR_INVALID_ARG;
     rc = sd_check_pointer(cache->d_k);
     if (rc != SD_OK) return rc;
-    const CommitArgs a = {*cache, *rows, d_path, d_new_cached};
-    cudaStream_t st = (cudaStream_t)stream;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(rows->n, 2 * cache->n_layers); cfg.blockDim = dim3(128); cfg.stream = st;
-    cfg.attrs = &attr; cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, commit_kernel, a) != cudaSuccess) return SD_ERR_CUDA;
-    return sd_launch(lengths_kernel, (rows->n + 127) / 128, 128, 0, st, a) == cudaSuccess ? SD_OK : SD_ERR_CUDA;
+    // Eight blocks a request, fewer where there is not so much to move.
+    const long long pieces = 2ll * cache->n_layers * cache->kv_heads * (cache->head_dim / 8);
+    if (pieces > 0x7FFFFFFF / 2) return SD_ERR_INVALID_ARG;
+    int blocks = 1;
+    while (blocks < 8 && pieces > blocks * COMMIT_THREADS) blocks *= 2;
+    if ((long long)rows->n * blocks > 0x7FFFFFFF) return SD_ERR_INVALID_ARG;
+    const CommitArgs a = {*cache, *rows, d_path, d_new_cached, blocks};
+    return sd_launch_clusters(commit_kernel, (unsigned)rows->n * blocks, blocks, COMMIT_THREADS, 0, (cudaStream_t)stream, a) == cudaSuccess ? SD_OK : SD_ERR_CUDA;
 }
