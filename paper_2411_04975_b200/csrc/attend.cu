@@ -21,7 +21,7 @@ namespace {
 
 constexpr int TILE = 128;                                         // lines of the cache a step
 constexpr int THREADS = 384;                                      // four warps that feed, eight that compute
-constexpr int UNITS = 2;                                          // units that the list's walker is ahead
+constexpr int UNITS = 3;                                          // units that are known: the one at work and two more
 constexpr int LEAST = 4;                                          // of a block's piece: a shorter one costs more to join than it saves
 constexpr float RESCALE = 8.0f;                                   // results are rescaled when a row's maximum has grown by 2^8 (weights stay below that)
 
@@ -483,6 +483,19 @@ __device__ __noinline__ void add_lines(const uint32_t* lines, const uint8_t* val
 }
 
 // ---- softmax -------------------------------------------------------------------------------
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+
+// Two weights in the type of the values.  They are not negative, so that for bf16 half a step can be added to their bits (a tie goes up); the conversion
+// instruction shares a pipe with the powers of two.
+template <class T> __device__ __forceinline__ uint32_t weights(float2 p);
+template <> __device__ __forceinline__ uint32_t weights<__nv_bfloat16>(float2 p) { return __byte_perm(__float_as_uint(p.x) + 0x8000u, __float_as_uint(p.y) + 0x8000u, 0x7632); }
+template <> __device__ __forceinline__ uint32_t weights<__half>(float2 p) { return Elem<__half>::down(p.x, p.y); }
+
+// What is needed of a tile that not every row sees whole: which of its lines this row sees, and lines with values that are no numbers.
+struct Border {
+    uint32_t words[4], lines;
+};
+
 template <class T, int D>
 struct Softmax {
     using S = Shape<D>;
@@ -495,55 +508,63 @@ struct Softmax {
     const int my_row, my_head;                                    // of the tile's rows, of the group's heads
     uint32_t meets = 0, group_meets = 0, s_count = 0, o_count0 = 0, o_count1 = 0, it = 0;
 
-    __device__ __forceinline__ bool meet() { bw_arrive_warp(bw_smem(&s->meet)); return bw_wait_warp(bw_smem(&s->meet), meets++ & 1, &s->stop); }
+    __device__ __forceinline__ bool meet() { return meet_of(true); }
     __device__ __forceinline__ bool meet_of(bool both) {
         const uint32_t bar = bw_smem(both ? &s->meet : &s->group_meet[w]), parity = (both ? meets++ : group_meets++) & 1;
         bw_arrive_warp(bar);
         return bw_wait_warp(bar, parity, &s->stop);
     }
     __device__ bool run(int n);
+    __device__ bool finish(const Unit& u, float top, float sum, bool row, bool busy, int r);
 };
+
+// The group's (both: both groups') look at a tile of values.
+template <class T, int D>
+__device__ __noinline__ Border border_of(const AttendArgs& a, const Unit* u, bool row, int r, int place, uint32_t* group_lines, const uint8_t* values, int t) {
+    Sight see = {0, 0, u->cached, false, 0ull};
+    if (row) see = sight_of(a.b, u->request, u->cached, u->count, u->row0 + r, a.p.window, a.p.sinks);
+    __syncwarp();
+    Border e;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) e.words[c] = see.word(place + 32 * c);
+    const uint32_t of_warp = lines_without_numbers<T, D>(values, t);
+    if ((t & 31) == 0) group_lines[t >> 5] = of_warp;
+    return e;
+}
 
 template <class T, int D>
 __device__ bool Softmax<T, D>::run(int n) {
-    const Unit& v = s->units[n % UNITS];
-    const int kind = v.kind, request = v.request, head = v.head, urows = v.rows, row0 = v.row0, cached = v.cached, count = v.count, k0 = v.k0, tiles = v.k1 - v.k0,
-              sink_tiles = v.sink_tiles, next_tile = v.next_tile, to = v.to, slot = v.slot;
-    const long long begin = v.begin;
-    bw_arrive_warp(bw_smem(&s->unit_empty[n % UNITS]));
-    if (kind == DONE) return false;
-    const bool wide = urows > a.tile_rows;
-    const int jobs = wide ? 2 * tiles : tiles;
+    const Unit& u = s->units[n % UNITS];
+    if (u.kind == DONE) return false;
+    const bool wide = u.rows > a.tile_rows;
+    const int tiles = u.k1 - u.k0, jobs = wide ? 2 * tiles : tiles;
     const int r = (wide ? w * a.tile_rows : 0) + my_row;          // of the unit's rows
-    const bool row = my_row < a.tile_rows && r < urows;
+    const bool row = my_row < a.tile_rows && r < u.rows;
     const bool busy = __any_sync(~0u, row);                       // any row of the warp
+    // tiles that every row sees whole: up to plain_end, but of those not the ones from sinks_end to plain_from
+    const int W = a.p.window;
+    const int plain_end = u.kind == PREFIX ? 0x7FFFFFFF : u.cached / TILE, plain_from = W ? max(0, u.cached + SD_MAX_SPEC - W + TILE) / TILE : 0, sinks_end = W ? min(a.p.sinks, u.cached) / TILE : 0;
+    const int k0 = u.k0, sink_tiles = u.sink_tiles, behind = u.next_tile - sink_tiles;
     if (!meet()) return false;                                    // both groups are through with the results of the unit before
     if (t == 0) s->begun[w] = 0;
-    // tiles that every row sees whole
-    const int W = a.p.window, plain_from = W ? cached + SD_MAX_SPEC - W + 1 : 0, plain_sinks = W ? min(a.p.sinks, cached) : 0;
     const uint32_t S0 = tmem + w * TILE, O0 = tmem + 2 * TILE + w * TILE;
     const float scale = a.scale;
     float top = -INFINITY, sum = 0.f;                             // the row's reference for powers, and its sum
 
 #pragma unroll 1
     for (int j = w; j < jobs; j += 2) {
-        const int tile = wide ? j >> 1 : j, k = k0 + tile;
-        const int p0 = TILE * (k < sink_tiles ? k : next_tile + k - sink_tiles);
-        const bool masked = kind == TAIL && !(p0 + TILE <= cached && (p0 >= plain_from || p0 + TILE <= plain_sinks));
-        uint32_t words[4], lines = 0;
-        const uint32_t vs = it + 2 * tile + 1;
-        uint8_t* values = base + S::RING + vs % S::SLOTS * S::SLOT_BYTES;
+        const int k = k0 + (wide ? j >> 1 : j), number = k < sink_tiles ? k : k + behind;
+        const bool masked = number >= plain_end || (number < plain_from && number >= sinks_end);
+        Border border;
+        border.lines = 0;
+        uint8_t* values = base;
         if (masked) {
-            Sight see = {0, 0, cached, false, 0ull};
-            if (row) see = sight_of(a.b, request, cached, count, row0 + r, W, a.p.sinks);
-            __syncwarp();
-#pragma unroll
-            for (int c = 0; c < 4; ++c) words[c] = see.word(p0 + 32 * c);
+            const uint32_t vs = it + 2 * (wide ? j >> 1 : j) + 1;
+            values += S::RING + vs % S::SLOTS * S::SLOT_BYTES;
             if (!bw_wait_warp(bw_smem(&s->full[vs % S::SLOTS]), (vs / S::SLOTS) & 1, &s->stop)) return false;
-            const uint32_t of_warp = lines_without_numbers<T, D>(values, t);
-            if ((t & 31) == 0) s->lines[w][t >> 5] = of_warp;
+            border = border_of<T, D>(a, &u, row, r, number * TILE, s->lines[w], values, t);
             if (!meet_of(wide)) return false;
-            lines = s->lines[w][0] | s->lines[w][1] | s->lines[w][2] | s->lines[w][3];
+            border.lines = s->lines[w][0] | s->lines[w][1] | s->lines[w][2] | s->lines[w][3];
         }
         if (!bw_wait_warp(bw_smem(&s->s_full[w]), s_count++ & 1, &s->stop)) return false;
         bw_fence_after();
@@ -560,35 +581,38 @@ __device__ bool Softmax<T, D>::run(int n) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[32 * c + e] = words[c] >> e & 1 ? x[32 * c + e] : 0xFF800000u;
+                        for (int e = 0; e < 32; ++e) x[32 * c + e] = border.words[c] >> e & 1 ? x[32 * c + e] : 0xFF800000u;
                 float m[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) m[q] = __uint_as_float(x[q]);
 #pragma unroll
-                for (int e = 4; e < TILE; e += 8)
+                for (int e = 4; e + 8 <= TILE; e += 8)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        m[q] = fmaxf(m[q], e + 4 + q < TILE ? fmaxf(__uint_as_float(x[e + q]), __uint_as_float(x[e + 4 + q])) : __uint_as_float(x[e + q]));
+                    for (int q = 0; q < 4; ++q) m[q] = max3(m[q], __uint_as_float(x[e + q]), __uint_as_float(x[e + 4 + q]));
+#pragma unroll
+                for (int q = 0; q < 4; ++q) m[q] = fmaxf(m[q], __uint_as_float(x[TILE - 4 + q]));
                 const float mx = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
                 const bool up = mx != -INFINITY && !((mx - top) * scale <= RESCALE);
-                const float alpha = up ? ex2((top - mx) * scale) : 1.f;
-                if (up) top = mx;
-                sum *= alpha;
-                power = (top == -INFINITY ? 0.f : top * scale) - BIAS;
-                if (j >= 2 && __any_sync(~0u, up)) {
+                if (__any_sync(~0u, up)) {
+                    const float alpha = up ? ex2((top - mx) * scale) : 1.f;
+                    if (up) top = mx;
+                    sum *= alpha;
+                    if (j >= 2) {
 #pragma unroll 1
-                    for (int c = 0; c < D; c += 16) {
-                        uint32_t y[16];
-                        bw_ld16(O0 + c, y);
-                        bw_wait_ld16(y);
+                        for (int c = 0; c < D; c += 16) {
+                            uint32_t y[16];
+                            bw_ld16(O0 + c, y);
+                            bw_wait_ld16(y);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * alpha);
-                        bw_st16(O0 + c, y);
+                            for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * alpha);
+                            bw_st16(O0 + c, y);
+                        }
                     }
                 }
+                power = (top == -INFINITY ? 0.f : top * scale) - BIAS;
             }
-            if (!lines) break;
-            if (busy) add_lines<T, D>(s->lines[w], values, S0, O0, j < 2, words[0], words[1], words[2], words[3], scale, power);
+            if (!border.lines) break;
+            if (busy) add_lines<T, D>(s->lines[w], values, S0, O0, j < 2, border.words[0], border.words[1], border.words[2], border.words[3], scale, power);
             if (j < 2 && t == 0) s->begun[w] = 1;
             if (!meet_of(wide)) return false;
             if ((s->lines[w][t >> 5] >> (t & 31) & 1) && (w == 0 || !wide)) {
@@ -598,7 +622,7 @@ __device__ bool Softmax<T, D>::run(int n) {
             }
             __syncwarp();
             if (wide && !meet()) return false;
-            lines = 0;                                            // (and the scores again: nothing is kept in registers over this)
+            border.lines = 0;                                     // (and the scores again: nothing is kept in registers over this)
         }
         if (busy) {
             const float2 by = make_float2(scale, scale), less = make_float2(-power, -power);
@@ -608,9 +632,9 @@ __device__ bool Softmax<T, D>::run(int n) {
                 const float2 z = sd_fma2(make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), by, less);
                 const float2 p = make_float2(ex2(z.x), ex2(z.y));
                 part[e / 2 % 2] = sd_add2(part[e / 2 % 2], p);
-                x[e / 2] = Elem<T>::down(p.x, p.y);
+                x[e / 2] = weights<T>(p);
+                if (e == TILE / 2 - 2) bw_st32(S0, x);
             }
-            bw_st32(S0, x);
             bw_st32(S0 + 32, x + 32);
             sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
         }
@@ -618,12 +642,20 @@ __device__ bool Softmax<T, D>::run(int n) {
         bw_fence_before();
         bw_arrive_warp(bw_smem(&s->p_ready[w]));
     }
+    if (!finish(u, top, sum, row, busy, r)) return false;
+    it += 2 * tiles;
+    bw_arrive_warp(bw_smem(&s->unit_empty[n % UNITS]));
+    return true;
+}
 
-    // ---- results: O[A] * g0, with the other group's part O[A + TILE] * g1 where both have one
-    float g0, g1 = 0.f, m = top, l = sum;
+// A unit's results: O[A] * g0, with the other group's part O[A + TILE] * g1 where both have one.
+template <class T, int D>
+__device__ __forceinline__ bool Softmax<T, D>::finish(const Unit& u, float top, float sum, bool row, bool busy, int r) {
+    const bool wide = u.rows > a.tile_rows, two = !wide && u.k1 - u.k0 > 1;
+    const float scale = a.scale;
+    float g0 = 1.f, g1 = 0.f, m = top, l = sum;
     int c0 = 0, c1 = D;
-    uint32_t A = O0;
-    const bool two = !wide && jobs > 1;
+    uint32_t A = tmem + 2 * TILE + w * TILE;
     if (!wide) {
         s->sums[w][t] = make_float2(top, sum);
         if (!meet()) return false;
@@ -633,6 +665,7 @@ __device__ bool Softmax<T, D>::run(int n) {
     ++o_count0;
     o_count1 += wide || two;
     bw_fence_after();
+    if (!busy) return true;
     if (!wide) {
         const float2 x0 = s->sums[0][t], x1 = s->sums[1][t];
         m = two ? fmaxf(x0.x, x1.x) : x0.x;
@@ -642,50 +675,45 @@ __device__ bool Softmax<T, D>::run(int n) {
         l = x0.y * g0 + (two ? x1.y * g1 : 0.f);
         A = tmem + 2 * TILE;
         c0 = w * (D / 2); c1 = c0 + D / 2;
-    } else {
-        g0 = 1.f;
     }
     const float inv = l == 0.f ? 0.f : rcp(l);
     g0 *= inv;
     g1 *= inv;
-    if (busy) {
-        const long long at = (begin + r) * a.p.q_heads + head * a.group + my_head;      // row and query head
-        const int mrow = (wide ? w * 128 : 0) + t;
-        T* out = (T*)a.out + (begin + r) * a.p.out_stride[0] + (head * a.group + my_head) * a.p.out_stride[1];
-        float* part = to == SLOT ? a.part + ((long long)slot * 256 + mrow) * D : a.plane[slot & 1] + at * D;
+    const int h = u.head * a.group + my_head, to = u.to, mrow = (wide ? w * 128 : 0) + t;
+    const long long at = (u.begin + r) * a.p.q_heads + h;         // row and query head
+    T* out = (T*)a.out + (u.begin + r) * a.p.out_stride[0] + h * a.p.out_stride[1];
+    float* part = to == SLOT ? a.part + ((long long)u.slot * 256 + mrow) * D : a.plane[u.slot & 1] + at * D;
 #pragma unroll 1
-        for (int c = c0; c < c1; c += 16) {
-            uint32_t x[16], z[16];
-            bw_ld16(A + c, x);
-            if (two) bw_ld16(A + TILE + c, z);
-            bw_wait_ld16(x);
-            if (two) bw_wait_ld16(z);
-            float y[16];
+    for (int c = c0; c < c1; c += 16) {
+        uint32_t x[16], z[16];
+        bw_ld16(A + c, x);
+        if (two) bw_ld16(A + TILE + c, z);
+        bw_wait_ld16(x);
+        if (two) bw_wait_ld16(z);
+        float y[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {                        // (a part without a weight may hold anything)
-                y[e] = g0 == 0.f ? 0.f : __uint_as_float(x[e]) * g0;
-                if (two && g1 != 0.f) y[e] += __uint_as_float(z[e]) * g1;
-            }
-            if (row) {
-                if (to == FINAL) {
-                    *(uint4*)(out + c) = sd_pack<T>(y);
-                    *(uint4*)(out + c + 8) = sd_pack<T>(y + 8);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 16; e += 4) *(float4*)(part + c + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
-                }
-            }
-            __syncwarp();
+        for (int e = 0; e < 16; ++e) {                            // (a part without a weight may hold anything)
+            y[e] = g0 == 0.f ? 0.f : __uint_as_float(x[e]) * g0;
+            if (two && g1 != 0.f) y[e] += __uint_as_float(z[e]) * g1;
         }
-        if (row && (wide || w == 0)) {
-            const float lse = l == 0.f ? -INFINITY : m * scale + lg2(l) - BIAS;
-            if (to != FINAL) *(to == SLOT ? a.part_lse + (long long)slot * 256 + mrow : a.plane_lse[slot & 1] + at) = lse;
-            else if (a.lse) a.lse[at] = lse * 0.69314718055994531f;
+        if (row) {
+            if (to == FINAL) {
+                *(uint4*)(out + c) = sd_pack<T>(y);
+                *(uint4*)(out + c + 8) = sd_pack<T>(y + 8);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) *(float4*)(part + c + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+            }
         }
         __syncwarp();
     }
+    if (row && (wide || w == 0)) {
+        const float lse = l == 0.f ? -INFINITY : m * scale + lg2(l) - BIAS;
+        if (to != FINAL) *(to == SLOT ? a.part_lse + (long long)u.slot * 256 + mrow : a.plane_lse[u.slot & 1] + at) = lse;
+        else if (a.lse) a.lse[at] = lse * 0.69314718055994531f;
+    }
+    __syncwarp();
     bw_fence_before();
-    it += 2 * tiles;
     return true;
 }
 
@@ -772,7 +800,7 @@ __device__ void join_row(const AttendArgs& a, const Cut& c, int m, int lane, boo
         top = most;
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] *= keep;
-#pragma unroll 4
+#pragma unroll 8
         for (int k = 0; k < n; ++k) {
             const float* y = a.part + slot(first + k) * D + lane * E;
             const float g = __shfl_sync(~0u, f, k);
@@ -938,7 +966,7 @@ int launch(const AttendArgs& a, const Room& r, cudaStream_t st) {
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(r.blocks, 4); cfg.blockDim = dim3(32 * JOIN_ROWS); cfg.stream = st;
+    cfg.gridDim = dim3(r.blocks, std::min((std::min(a.b.max_draft + 1, 2 * a.tile_rows) * a.group + JOIN_ROWS - 1) / JOIN_ROWS, 16)); cfg.blockDim = dim3(32 * JOIN_ROWS); cfg.stream = st;
     cfg.attrs = &attr; cfg.numAttrs = 1;
     SD_CUDA_OK(cudaLaunchKernelEx(&cfg, join_cuts_kernel<T, D>, a, r.planes));
     if (r.planes) SD_CUDA_OK(sd_launch(join_planes_kernel<T, D>, a.b.rows, 256, 0, st, a));
