@@ -23,6 +23,7 @@ constexpr int TILE = 128;                                         // lines of th
 constexpr int THREADS = 384;                                      // four warps that feed, eight that compute
 constexpr int UNITS = 3;                                          // units that are known: the one at work and two more
 constexpr int LEAST = 4;                                          // of a block's piece: a shorter one costs more to join than it saves
+constexpr float BIAS_FP16 = 7.0f;                                 // fp16 weights are 2^7 as large: more of the small ones are above its least number
 constexpr float RESCALE = 8.0f;                                   // results are rescaled when a row's maximum has grown by 2^8 (weights stay below that)
 
 struct Cut {
@@ -439,9 +440,9 @@ __device__ __forceinline__ uint32_t lines_without_numbers(const uint8_t* values,
     return __ballot_sync(~0u, found != 0);
 }
 
-// S0, O0: the warp's scores and results.  words: what the row sees.  first: the results begin here.
+// S0, O0: the warp's scores and results.  first: the results begin here.
 template <class T, int D>
-__device__ __noinline__ void add_lines(const uint32_t* lines, const uint8_t* values, uint32_t S0, uint32_t O0, bool first, uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3, float scale, float power) {
+__device__ __noinline__ void add_lines(const uint32_t* lines, const uint8_t* values, uint32_t S0, uint32_t O0, bool first, const Sight& see, int place, float scale, float power) {
     if (first)
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
@@ -453,7 +454,8 @@ __device__ __noinline__ void add_lines(const uint32_t* lines, const uint8_t* val
     bw_wait_st();
 #pragma unroll 1
     for (int c = 0; c < 4; ++c) {
-        const uint32_t word = c == 0 ? w0 : c == 1 ? w1 : c == 2 ? w2 : w3;
+        const uint32_t word = see.word(place + 32 * c);
+        __syncwarp();
 #pragma unroll 1
         for (uint32_t left = lines[c]; left; left &= left - 1) {
             const int l = 32 * c + __ffs(left) - 1;
@@ -491,15 +493,10 @@ template <class T> __device__ __forceinline__ uint32_t weights(float2 p);
 template <> __device__ __forceinline__ uint32_t weights<__nv_bfloat16>(float2 p) { return __byte_perm(__float_as_uint(p.x) + 0x8000u, __float_as_uint(p.y) + 0x8000u, 0x7632); }
 template <> __device__ __forceinline__ uint32_t weights<__half>(float2 p) { return Elem<__half>::down(p.x, p.y); }
 
-// What is needed of a tile that not every row sees whole: which of its lines this row sees, and lines with values that are no numbers.
-struct Border {
-    uint32_t words[4], lines;
-};
-
 template <class T, int D>
 struct Softmax {
     using S = Shape<D>;
-    static constexpr float BIAS = IsBf16<T>::v ? 0.0f : 7.0f;     // fp16 weights are 2^7 as large: more of the small ones are above its least number
+    static constexpr float BIAS = IsBf16<T>::v ? 0.0f : BIAS_FP16;
     const AttendArgs& a;
     Rest* s;
     uint8_t* base;                                                // of shared memory
@@ -518,18 +515,92 @@ struct Softmax {
     __device__ bool finish(const Unit& u, float top, float sum, bool row, bool busy, int r);
 };
 
-// The group's (both: both groups') look at a tile of values.
-template <class T, int D>
-__device__ __noinline__ Border border_of(const AttendArgs& a, const Unit* u, bool row, int r, int place, uint32_t* group_lines, const uint8_t* values, int t) {
-    Sight see = {0, 0, u->cached, false, 0ull};
-    if (row) see = sight_of(a.b, u->request, u->cached, u->count, u->row0 + r, a.p.window, a.p.sinks);
-    __syncwarp();
-    Border e;
+// The warp's results times alpha.  (Seldom: out of line.)
+template <int D>
+__device__ __noinline__ void scale_results(uint32_t O0, float alpha) {
+#pragma unroll 1
+    for (int c = 0; c < D; c += 16) {
+        uint32_t y[16];
+        bw_ld16(O0 + c, y);
+        bw_wait_ld16(y);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) e.words[c] = see.word(place + 32 * c);
-    const uint32_t of_warp = lines_without_numbers<T, D>(values, t);
-    if ((t & 31) == 0) group_lines[t >> 5] = of_warp;
-    return e;
+        for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * alpha);
+        bw_st16(O0 + c, y);
+    }
+    bw_wait_st();
+}
+
+// A tile that not every row sees whole.  Scores that a row does not see become -inf, in tensor memory, so that the rest is the same for all tiles; and if lines of the
+// values hold no numbers, the row's reference is brought up to date, their part is added to the results and they are cleared (see above).
+// Out of line: in the loop over tiles its instructions and registers cost whole tiles a quarter of their time.
+struct Border {
+    uint8_t* values;
+    uint32_t S0, O0, s_full, s_parity, v_full, v_parity, meets, group_meets;
+    Sight see;
+    int w, t, place;
+    bool busy, first, both;
+    float top, sum;
+};
+
+template <class T, int D>
+__device__ __noinline__ bool border_tile(const AttendArgs& a, Rest* s, Border& b) {
+    using S = Shape<D>;
+    auto meet = [&](bool both) {
+        const uint32_t bar = bw_smem(both ? &s->meet : &s->group_meet[b.w]), parity = (both ? b.meets++ : b.group_meets++) & 1;
+        bw_arrive_warp(bar);
+        return bw_wait_warp(bar, parity, &s->stop);
+    };
+    const Sight see = b.see;
+    if (!bw_wait_warp(b.v_full, b.v_parity, &s->stop)) return false;
+    const uint32_t of_warp = lines_without_numbers<T, D>(b.values, b.t);
+    if ((b.t & 31) == 0) s->lines[b.w][b.t >> 5] = of_warp;
+    if (!meet(b.both)) return false;
+    const uint32_t lines = s->lines[b.w][0] | s->lines[b.w][1] | s->lines[b.w][2] | s->lines[b.w][3];
+    if (!bw_wait_warp(b.s_full, b.s_parity, &s->stop)) return false;
+    bw_fence_after();
+    if (b.busy) {
+        float mx = -INFINITY;
+        bool sees = false;                                        // a line without numbers
+#pragma unroll 1
+        for (int c = 0; c < TILE; c += 64) {
+            uint32_t x[64];
+            bw_ld32(b.S0 + c, x);
+            bw_ld32(b.S0 + c + 32, x + 32);
+            const uint32_t words[2] = {see.word(b.place + c), see.word(b.place + c + 32)};
+            sees |= (words[0] & s->lines[b.w][c / 32]) | (words[1] & s->lines[b.w][c / 32 + 1]);
+            __syncwarp();
+            bw_wait_ld32(x);
+            bw_wait_ld32(x + 32);
+#pragma unroll
+            for (int e = 0; e < 64; ++e) {
+                x[e] = words[e / 32] >> e % 32 & 1 ? x[e] : 0xFF800000u;
+                mx = fmaxf(mx, __uint_as_float(x[e]));
+            }
+            bw_st32(b.S0 + c, x);
+            bw_st32(b.S0 + c + 32, x + 32);
+        }
+        bw_wait_st();
+        if (lines && (b.first || __any_sync(~0u, sees))) {        // (the reference by the rule of whole tiles: what nobody sees changes no bit)
+            const bool up = mx != -INFINITY && !((mx - b.top) * a.scale <= RESCALE);
+            const float alpha = up ? ex2((b.top - mx) * a.scale) : 1.f;
+            if (up) b.top = mx;
+            b.sum *= alpha;
+            __syncwarp();
+            if (!b.first) scale_results<D>(b.O0, alpha);
+            const float power = (b.top == -INFINITY ? 0.f : b.top * a.scale) - (IsBf16<T>::v ? 0.0f : BIAS_FP16);
+            add_lines<T, D>(s->lines[b.w], b.values, b.S0, b.O0, b.first, see, b.place, a.scale, power);
+        }
+    }
+    if (!lines) return true;
+    if (b.first && b.t == 0) s->begun[b.w] = 1;
+    if (!meet(b.both)) return false;
+    if ((s->lines[b.w][b.t >> 5] >> (b.t & 31) & 1) && (b.w == 0 || !b.both)) {
+#pragma unroll 1
+        for (int c = 0; c < D / 8; ++c) *(uint4*)(b.values + b.t * 128 + c / 8 * S::HALF_BYTES + c % 8 * 16) = make_uint4(0, 0, 0, 0);
+        bw_fence_async();
+    }
+    __syncwarp();
+    return b.both ? meet(true) : true;
 }
 
 template <class T, int D>
@@ -545,6 +616,8 @@ __device__ bool Softmax<T, D>::run(int n) {
     const int W = a.p.window;
     const int plain_end = u.kind == PREFIX ? 0x7FFFFFFF : u.cached / TILE, plain_from = W ? max(0, u.cached + SD_MAX_SPEC - W + TILE) / TILE : 0, sinks_end = W ? min(a.p.sinks, u.cached) / TILE : 0;
     const int k0 = u.k0, sink_tiles = u.sink_tiles, behind = u.next_tile - sink_tiles;
+    Sight see = {0, 0, u.cached, false, 0ull};
+    if (row && u.kind == TAIL) see = sight_of(a.b, u.request, u.cached, u.count, u.row0 + r, W, a.p.sinks);
     if (!meet()) return false;                                    // both groups are through with the results of the unit before
     if (t == 0) s->begun[w] = 0;
     const uint32_t S0 = tmem + w * TILE, O0 = tmem + 2 * TILE + w * TILE;
@@ -555,74 +628,42 @@ __device__ bool Softmax<T, D>::run(int n) {
     for (int j = w; j < jobs; j += 2) {
         const int k = k0 + (wide ? j >> 1 : j), number = k < sink_tiles ? k : k + behind;
         const bool masked = number >= plain_end || (number < plain_from && number >= sinks_end);
-        Border border;
-        border.lines = 0;
-        uint8_t* values = base;
         if (masked) {
             const uint32_t vs = it + 2 * (wide ? j >> 1 : j) + 1;
-            values += S::RING + vs % S::SLOTS * S::SLOT_BYTES;
-            if (!bw_wait_warp(bw_smem(&s->full[vs % S::SLOTS]), (vs / S::SLOTS) & 1, &s->stop)) return false;
-            border = border_of<T, D>(a, &u, row, r, number * TILE, s->lines[w], values, t);
-            if (!meet_of(wide)) return false;
-            border.lines = s->lines[w][0] | s->lines[w][1] | s->lines[w][2] | s->lines[w][3];
+            Border b = {base + S::RING + vs % S::SLOTS * S::SLOT_BYTES, S0, O0, bw_smem(&s->s_full[w]), s_count & 1, bw_smem(&s->full[vs % S::SLOTS]), (vs / S::SLOTS) & 1,
+                        meets, group_meets, see, w, t, number * TILE, busy, j < 2, wide, top, sum};
+            if (!border_tile<T, D>(a, s, b)) return false;
+            meets = b.meets; group_meets = b.group_meets; top = b.top; sum = b.sum;
+        } else {
+            if (!bw_wait_warp(bw_smem(&s->s_full[w]), s_count & 1, &s->stop)) return false;
+            bw_fence_after();
         }
-        if (!bw_wait_warp(bw_smem(&s->s_full[w]), s_count++ & 1, &s->stop)) return false;
-        bw_fence_after();
+        ++s_count;
         uint32_t x[TILE];
         float power = 0.f;
-#pragma unroll 1
-        for (;;) {
-            if (busy) {
+        if (busy) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) bw_ld32(S0 + 32 * c, x + 32 * c);
+            for (int c = 0; c < 4; ++c) bw_ld32(S0 + 32 * c, x + 32 * c);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) bw_wait_ld32(x + 32 * c);
-                if (masked)
+            for (int c = 0; c < 4; ++c) bw_wait_ld32(x + 32 * c);
+            float m[4];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+            for (int q = 0; q < 4; ++q) m[q] = __uint_as_float(x[q]);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[32 * c + e] = border.words[c] >> e & 1 ? x[32 * c + e] : 0xFF800000u;
-                float m[4];
+            for (int e = 4; e + 8 <= TILE; e += 8)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) m[q] = __uint_as_float(x[q]);
+                for (int q = 0; q < 4; ++q) m[q] = max3(m[q], __uint_as_float(x[e + q]), __uint_as_float(x[e + 4 + q]));
 #pragma unroll
-                for (int e = 4; e + 8 <= TILE; e += 8)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) m[q] = max3(m[q], __uint_as_float(x[e + q]), __uint_as_float(x[e + 4 + q]));
-#pragma unroll
-                for (int q = 0; q < 4; ++q) m[q] = fmaxf(m[q], __uint_as_float(x[TILE - 4 + q]));
-                const float mx = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-                const bool up = mx != -INFINITY && !((mx - top) * scale <= RESCALE);
-                if (__any_sync(~0u, up)) {
-                    const float alpha = up ? ex2((top - mx) * scale) : 1.f;
-                    if (up) top = mx;
-                    sum *= alpha;
-                    if (j >= 2) {
-#pragma unroll 1
-                        for (int c = 0; c < D; c += 16) {
-                            uint32_t y[16];
-                            bw_ld16(O0 + c, y);
-                            bw_wait_ld16(y);
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * alpha);
-                            bw_st16(O0 + c, y);
-                        }
-                    }
-                }
-                power = (top == -INFINITY ? 0.f : top * scale) - BIAS;
+            for (int q = 0; q < 4; ++q) m[q] = fmaxf(m[q], __uint_as_float(x[TILE - 4 + q]));
+            const float mx = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+            const bool up = mx != -INFINITY && !((mx - top) * scale <= RESCALE);
+            if (__any_sync(~0u, up)) {
+                const float alpha = up ? ex2((top - mx) * scale) : 1.f;
+                if (up) top = mx;
+                sum *= alpha;
+                if (j >= 2) scale_results<D>(O0, alpha);
             }
-            if (!border.lines) break;
-            if (busy) add_lines<T, D>(s->lines[w], values, S0, O0, j < 2, border.words[0], border.words[1], border.words[2], border.words[3], scale, power);
-            if (j < 2 && t == 0) s->begun[w] = 1;
-            if (!meet_of(wide)) return false;
-            if ((s->lines[w][t >> 5] >> (t & 31) & 1) && (w == 0 || !wide)) {
-#pragma unroll 1
-                for (int c = 0; c < D / 8; ++c) *(uint4*)(values + t * 128 + c / 8 * S::HALF_BYTES + c % 8 * 16) = make_uint4(0, 0, 0, 0);
-                bw_fence_async();
-            }
-            __syncwarp();
-            if (wide && !meet()) return false;
-            border.lines = 0;                                     // (and the scores again: nothing is kept in registers over this)
+            power = (top == -INFINITY ? 0.f : top * scale) - BIAS;
         }
         if (busy) {
             const float2 by = make_float2(scale, scale), less = make_float2(-power, -power);
