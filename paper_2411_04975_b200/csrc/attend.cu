@@ -6,8 +6,8 @@
 // falls so, so that every multiprocessor reads as much of the cache as any other, whatever the lengths; each block finds its piece from the lengths by itself.
 // Rows of a unit that was cut are left as partial results (normalised, with the logarithm of their sum) and joined by a second kernel.
 //
-// A block is a warp that copies keys and values into a ring in shared memory, one that issues the products, one that walks the list, one that copies
-// queries, and two groups of four warps that compute the softmax, a thread per packed row.  Two chains of (scores, softmax, product with the values)
+// A block is a warp that copies keys and values into a ring in shared memory, one that walks the list and copies queries, and two groups of four warps that
+// compute the softmax, a thread per packed row, each with a warp that issues its products.  Two chains of (scores, softmax, product with the values)
 // are in flight, one per group: for a unit of up to 128 rows the groups take tiles in turns and join their results at the end, for a larger one each has 128 rows of every tile.
 // While one group is at its softmax the tensor cores work for the other.  Scores and results are in tensor memory; the weights go back over the scores
 // and are read from there.
@@ -91,7 +91,7 @@ struct Shape {
 };
 
 struct Rest {                     // of shared memory
-    uint64_t full[8], empty[8], s_full[2], p_ready[2], o_done[2], q_full[2], q_empty[2], unit_full[UNITS], unit_empty[UNITS], meet, group_meet[2], over;
+    uint64_t full[8], empty[8], s_full[2], p_ready[2], o_done[2], q_full[2], q_empty[2], unit_full[UNITS], unit_empty[UNITS], meet, group_meet[2], over[2], lead;
     uint32_t tmem;
     int stop;
     int begun[2];                 // the group has begun its results itself: the first product adds to them
@@ -149,6 +149,15 @@ __device__ __noinline__ Sight sight_of(const sd_rows& b, int request, int cached
 template <class T> struct IsBf16 { static constexpr bool v = false; };
 template <> struct IsBf16<__nv_bfloat16> { static constexpr bool v = true; };
 
+// Given up: the copies in flight come to their end.
+__device__ __noinline__ void drain(uint64_t* full, uint32_t slots, uint32_t filled) {
+    for (uint32_t e = 0; e < slots && e < filled; ++e) {
+        const uint32_t last = (filled - 1 - e) / slots * slots + e;
+        int never = 0;
+        bw_wait_slow(bw_smem(&full[e]), (last / slots) & 1, &never, 200000000ll);
+    }
+}
+
 // ---- the list's walker ---------------------------------------------------------------------
 // What a request's units cost: their tiles, and one more each for a unit's begin and end.  (31 bits are enough: the host has seen to that.)
 struct Quote {
@@ -168,7 +177,9 @@ __device__ __noinline__ Quote quote_of(const AttendArgs& a, int prefix_tiles, in
     return e;
 }
 
-__device__ void walk_units(const AttendArgs& a, Rest* s, int lane) {
+template <int D>
+__device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, uint32_t q, int lane) {
+    using S = Shape<D>;
     const sd_rows& b = a.b;
     const int H = a.c.kv_heads, most = 2 * a.tile_rows;           // rows of a unit
     const int prefix_tiles = a.p.window ? 0 : a.p.shared / TILE;
@@ -199,6 +210,7 @@ __device__ void walk_units(const AttendArgs& a, Rest* s, int lane) {
     Cut cut;
     cut.first = 0; cut.last = -1;
     int at = 0, base = 0;                                         // units handed out; of the list, what is behind
+    uint32_t qi = 0;                                              // tiles of queries
     bool ok = true;
     // 32 requests at a time, then those of them that the piece touches, then their units
 #pragma unroll 1
@@ -251,6 +263,16 @@ __device__ void walk_units(const AttendArgs& a, Rest* s, int lane) {
                     bw_arrive(bw_smem(&s->unit_full[place]));
                 }
                 ++at;
+                // its queries: a tile's rows and heads in one copy for each half of the head; rows behind the unit's come along and are left alone
+#pragma unroll 1
+                for (int row = 0; row < u.rows && ok; row += a.tile_rows, ++qi) {
+                    const uint32_t slot = qi % 2, bar = bw_smem(&s->q_full[slot]);
+                    ok = qi < 2 || bw_wait_warp(bw_smem(&s->q_empty[slot]), (qi / 2 - 1) & 1, &s->stop);
+                    if (!ok || lane) continue;
+                    bw_arrive_expect(bar, S::HALVES * 128 * a.group * a.tile_rows);
+                    for (int h = 0; h < S::HALVES; ++h) bw_load_3d(q + slot * S::Q_BYTES + h * S::HALF_BYTES, mq, h * 64, u.head * a.group, (int)u.begin + row, bar);
+                }
+                if (!ok) break;
             }
         }
         base = __shfl_sync(~0u, end, 31);
@@ -261,11 +283,13 @@ __device__ void walk_units(const AttendArgs& a, Rest* s, int lane) {
         s->units[e].kind = DONE;
         bw_arrive(bw_smem(&s->unit_full[e]));
     }
+    if (!ok) drain(s->q_full, 2, qi);
 }
 
 // Pages that a request's rows see: told where one is none of the cache's.
 __device__ void write_status(const AttendArgs& a, int lane) {
     const sd_rows& b = a.b;
+#pragma unroll 1
     for (int i = blockIdx.x; i < b.n; i += gridDim.x) {
         const Request r = sd_request(b, i, a.c.page_size, a.p.shared);
         int st = r.status;
@@ -273,7 +297,9 @@ __device__ void write_status(const AttendArgs& a, int lane) {
             const int P = a.c.page_size, from = a.p.window ? max(0, r.cached - a.p.window + 1) : 0;
             const int sinks = a.p.window ? min(min(a.p.sinks, r.cached), from) : 0;
             bool bad = false;
+#pragma unroll 1
             for (int e = lane; e < (sinks + P - 1) / P; e += 32) bad |= sd_page(b, a.c.n_pages, i, e) < 0;
+#pragma unroll 1
             for (int e = from / P + lane; e <= (r.cached + r.count - 1) / P; e += 32) bad |= sd_page(b, a.c.n_pages, i, e) < 0;
             if (__any_sync(~0u, bad)) st |= SD_STATUS_BAD_PAGE;
         }
@@ -282,15 +308,6 @@ __device__ void write_status(const AttendArgs& a, int lane) {
 }
 
 // ---- copies --------------------------------------------------------------------------------
-// Given up: the copies in flight come to their end.
-__device__ __noinline__ void drain(uint64_t* full, uint32_t slots, uint32_t filled) {
-    for (uint32_t e = 0; e < slots && e < filled; ++e) {
-        const uint32_t last = (filled - 1 - e) / slots * slots + e;
-        int never = 0;
-        bw_wait_slow(bw_smem(&full[e]), (last / slots) & 1, &never, 200000000ll);
-    }
-}
-
 template <int D>
 __device__ void copy_lines(const AttendArgs& a, const CUtensorMap* mk, const CUtensorMap* mv, Rest* s, uint32_t ring, int lane) {
     using S = Shape<D>;
@@ -302,6 +319,7 @@ __device__ void copy_lines(const AttendArgs& a, const CUtensorMap* mk, const CUt
         if (!bw_wait_warp(bw_smem(&s->unit_full[n % UNITS]), (n / UNITS) & 1, &s->stop)) break;
         const Unit& v = s->units[n % UNITS];
         const int kind = v.kind, request = v.request, head = v.head, k0 = v.k0, k1 = v.k1, sink_tiles = v.sink_tiles, next_tile = v.next_tile;
+        const bool wide = v.rows > a.tile_rows;
         const int length = kind == PREFIX ? v.cached : v.cached + v.count;
         bw_arrive_warp(bw_smem(&s->unit_empty[n % UNITS]));
         if (kind == DONE) return;
@@ -323,7 +341,10 @@ __device__ void copy_lines(const AttendArgs& a, const CUtensorMap* mk, const CUt
                 const uint32_t e = it % S::SLOTS, bar = bw_smem(&s->full[e]);
                 ok = it < S::SLOTS || bw_wait_warp(bw_smem(&s->empty[e]), (it / S::SLOTS - 1) & 1, &s->stop);
                 if (!ok) break;
-                if (lane == 0) bw_arrive_expect(bar, boxes * box * 128);
+                if (lane == 0) {
+                    if (!wide) bw_arrive(bw_smem(&s->empty[e]));  // (for the group that does not use it)
+                    bw_arrive_expect(bar, boxes * box * 128);
+                }
                 __syncwarp();
                 if (page >= 0) bw_load_4d(ring + e * S::SLOT_BYTES + to, v ? mv : mk, half * 64, line, head, page, bar);
                 ++it;
@@ -335,81 +356,63 @@ __device__ void copy_lines(const AttendArgs& a, const CUtensorMap* mk, const CUt
     drain(s->full, S::SLOTS, it);
 }
 
-// Queries: a tile's rows and heads in one copy for each half of the head; rows behind the unit's come along and are left alone.
-template <int D>
-__device__ void copy_queries(const AttendArgs& a, const CUtensorMap* mq, Rest* s, uint32_t q, int lane) {
-    using S = Shape<D>;
-    uint32_t it = 0;
-    for (int n = 0;; ++n) {
-        if (!bw_wait_warp(bw_smem(&s->unit_full[n % UNITS]), (n / UNITS) & 1, &s->stop)) break;
-        const Unit& v = s->units[n % UNITS];
-        const int kind = v.kind, head = v.head, tiles = v.rows > a.tile_rows ? 2 : 1, begin = (int)v.begin;
-        bw_arrive_warp(bw_smem(&s->unit_empty[n % UNITS]));
-        if (kind == DONE) return;
-        bool ok = true;
-        for (int k = 0; k < tiles; ++k) {
-            const uint32_t e = it % 2, bar = bw_smem(&s->q_full[e]);
-            ok = it < 2 || bw_wait_warp(bw_smem(&s->q_empty[e]), (it / 2 - 1) & 1, &s->stop);
-            if (!ok) break;
-            if (lane == 0) {
-                bw_arrive_expect(bar, S::HALVES * 128 * a.group * a.tile_rows);
-                for (int h = 0; h < S::HALVES; ++h) bw_load_3d(q + e * S::Q_BYTES + h * S::HALF_BYTES, mq, h * 64, head * a.group, begin + k * a.tile_rows, bar);
-            }
-            ++it;
-        }
-        if (!ok) break;
-    }
-    drain(s->q_full, 2, it);
-}
-
 // ---- products ------------------------------------------------------------------------------
-// (One thread.)  False: given up.
+// (A warp for each group: to wait, to issue and to commit takes it as long as the products take.)  False: given up.
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(~0u, x, 0); }   // (the same in all lanes, and known to be)
+
 template <class T, int D>
-__device__ bool multiply(const AttendArgs& a, Rest* s, uint32_t ring, uint32_t q, uint32_t tmem) {
+__device__ bool multiply(const AttendArgs& a, Rest* s, uint32_t ring, uint32_t q, uint32_t tmem_, int w) {
     using S = Shape<D>;
     const uint32_t qk = bw_idesc(IsBf16<T>::v, 128, TILE, false) | (a.p.scale < 0.f ? 1u << 13 : 0u);   // (negated queries)
     constexpr uint32_t pv = bw_idesc(IsBf16<T>::v, 128, D, true);
-    uint32_t it = 0, qi = 0, count0 = 0, count1 = 0;
+    const uint32_t tmem = uniform(tmem_), S0 = tmem + w * TILE, O0 = tmem + 2 * TILE + w * TILE;
+    const bool leader = bw_elect();
+    uint32_t it = 0, qi = 0, count = 0, wides = 0;                // slots, queries, jobs, wide units behind
     for (int n = 0;; ++n) {
-        if (!bw_wait(bw_smem(&s->unit_full[n % UNITS]), (n / UNITS) & 1, &s->stop)) return false;
+        if (!bw_wait_warp(bw_smem(&s->unit_full[n % UNITS]), (n / UNITS) & 1, &s->stop)) return false;
         const Unit& u = s->units[n % UNITS];
-        const int kind = u.kind, tiles = u.k1 - u.k0;
-        const bool wide = u.rows > a.tile_rows;
-        bw_arrive(bw_smem(&s->unit_empty[n % UNITS]));
+        const int kind = uniform(u.kind), tiles = uniform(u.k1 - u.k0);
+        const bool wide = uniform(u.rows) > a.tile_rows;
+        bw_arrive_warp(bw_smem(&s->unit_empty[n % UNITS]));
         if (kind == DONE) return true;
-        const int jobs = wide ? 2 * tiles : tiles;
-        for (int k = 0; k < (wide ? 2 : 1); ++k)
-            if (!bw_wait(bw_smem(&s->q_full[(qi + k) % 2]), ((qi + k) / 2) & 1, &s->stop)) return false;
+        const int step = wide ? 1 : 2, first = wide ? 0 : w;      // the group's tiles
+        const uint32_t mine = (qi + (wide ? w : 0)) % 2;          // its queries
+        // Of a wide unit the second group begins when the first is halfway through its first tile: from then on the one computes while the other's products run.
+        if (wide && w && !bw_wait_warp(bw_smem(&s->lead), wides++ & 1, &s->stop)) return false;
+        for (int k = 0; k < (wide ? 2 : 1); ++k) {
+            const uint32_t e = (qi + k) % 2;
+            if (!bw_wait_warp(bw_smem(&s->q_full[e]), ((qi + k) / 2) & 1, &s->stop)) return false;
+            if (e != mine || first >= tiles) bw_arrive_warp(bw_smem(&s->q_empty[e]));   // (not used by this group)
+        }
 #pragma unroll 1
-        for (int j = -2; j < jobs; ++j) {                         // (scores are two ahead)
+        for (int j = first - step; j < tiles; j += step) {        // (scores are a tile ahead)
+            const int next = j + step;
+            const uint32_t v = it + 2 * j + 1, k = it + 2 * next;
             if (j >= 0) {
-                const int w = j & 1, tile = wide ? j >> 1 : j;
-                const uint32_t e = (it + 2 * tile + 1) % S::SLOTS;
-                if (!bw_wait(bw_smem(&s->full[e]), ((it + 2 * tile + 1) / S::SLOTS) & 1, &s->stop)) return false;
-                if (!bw_wait(bw_smem(&s->p_ready[w]), (w ? count1++ : count0++) & 1, &s->stop)) return false;
+                if (!bw_wait_warp(bw_smem(&s->full[v % S::SLOTS]), (v / S::SLOTS) & 1, &s->stop)) return false;
+                if (!bw_wait_warp(bw_smem(&s->p_ready[w]), count++ & 1, &s->stop)) return false;
                 bw_fence_after();
-                const bool add = j >= 2 || *(volatile int*)&s->begun[w];
-                const uint64_t vd = bw_desc_across(ring + e * S::SLOT_BYTES, S::HALF_BYTES);
+                const bool add = j >= step || uniform(*(volatile int*)&s->begun[w]);
+                const uint64_t vd = bw_desc_across(ring + v % S::SLOTS * S::SLOT_BYTES, S::HALF_BYTES);
 #pragma unroll
-                for (int k = 0; k < TILE / 16; ++k)
-                    bw_mma_ts(tmem + 2 * TILE + w * TILE, tmem + w * TILE + k * 8, vd + (k * 2048 >> 4), pv, add || k > 0);
-                if (!wide || w) bw_commit(bw_smem(&s->empty[e]));
-                if (j + 2 >= jobs) bw_commit(bw_smem(&s->o_done[w]));
+                for (int i = 0; i < TILE / 16; ++i) bw_mma_ts(O0, S0 + i * 8, vd + (i * 2048 >> 4), pv, add || i > 0, leader);
             }
-            if (j + 2 < jobs) {
-                const int i = j + 2, w = i & 1, tile = wide ? i >> 1 : i;
-                const uint32_t e = (it + 2 * tile) % S::SLOTS, qe = (qi + (wide ? w : 0)) % 2;
-                if (!bw_wait(bw_smem(&s->full[e]), ((it + 2 * tile) / S::SLOTS) & 1, &s->stop)) return false;
+            if (next < tiles) {
+                if (!bw_wait_warp(bw_smem(&s->full[k % S::SLOTS]), (k / S::SLOTS) & 1, &s->stop)) return false;
                 bw_fence_after();
-                const uint64_t qd = bw_desc(q + qe * S::Q_BYTES), kd = bw_desc(ring + e * S::SLOT_BYTES);
+                const uint64_t qd = bw_desc(q + mine * S::Q_BYTES), kd = bw_desc(ring + k % S::SLOTS * S::SLOT_BYTES);
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t off = (k / 4 * S::HALF_BYTES + k % 4 * 32) >> 4;
-                    bw_mma(tmem + w * TILE, qd + off, kd + off, qk, k > 0);
+                for (int i = 0; i < D / 16; ++i) {
+                    const uint32_t off = (i / 4 * S::HALF_BYTES + i % 4 * 32) >> 4;
+                    bw_mma(S0, qd + off, kd + off, qk, i > 0, leader);
                 }
-                bw_commit(bw_smem(&s->s_full[w]));
-                if (!wide || w) bw_commit(bw_smem(&s->empty[e]));
-                if (i >= jobs - (wide ? 2 : 1)) bw_commit(bw_smem(&s->q_empty[qe]));
+                bw_commit(bw_smem(&s->s_full[w]), leader);
+                bw_commit(bw_smem(&s->empty[k % S::SLOTS]), leader);
+                if (next + step >= tiles) bw_commit(bw_smem(&s->q_empty[mine]), leader);
+            }
+            if (j >= 0) {
+                bw_commit(bw_smem(&s->empty[v % S::SLOTS]), leader);
+                if (next >= tiles) bw_commit(bw_smem(&s->o_done[w]), leader);
             }
         }
         it += 2 * tiles;
@@ -432,7 +435,7 @@ template <class T, int D>
 __device__ __forceinline__ uint32_t lines_without_numbers(const uint8_t* values, int t) {
     const uint8_t* mine = values + t * 128;
     uint32_t found = 0;
-#pragma unroll
+#pragma unroll 4
     for (int c = 0; c < D / 8; ++c) {
         const uint4 x = *(const uint4*)(mine + c / 8 * Shape<D>::HALF_BYTES + ((c % 8) ^ (t & 7)) * 16);
         found |= no_number<T>(x.x) | no_number<T>(x.y) | no_number<T>(x.z) | no_number<T>(x.w);
@@ -445,11 +448,11 @@ template <class T, int D>
 __device__ __noinline__ void add_lines(const uint32_t* lines, const uint8_t* values, uint32_t S0, uint32_t O0, bool first, const Sight& see, int place, float scale, float power) {
     if (first)
 #pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-            uint32_t x[32];
+        for (int c = 0; c < D; c += 16) {
+            uint32_t x[16];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = 0;
-            bw_st32(O0 + c, x);
+            for (int e = 0; e < 16; ++e) x[e] = 0;
+            bw_st16(O0 + c, x);
         }
     bw_wait_st();
 #pragma unroll 1
@@ -463,12 +466,12 @@ __device__ __noinline__ void add_lines(const uint32_t* lines, const uint8_t* val
             if (!__any_sync(~0u, seen)) continue;
             const float p = ex2(fmaf(__uint_as_float(bw_ld1(S0 + l)), scale, -power));
 #pragma unroll 1
-            for (int d = 0; d < D; d += 32) {
-                uint32_t x[32];
-                bw_ld32(O0 + d, x);
-                bw_wait_ld32(x);
+            for (int d = 0; d < D; d += 16) {
+                uint32_t x[16];
+                bw_ld16(O0 + d, x);
+                bw_wait_ld16(x);
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
+                for (int e = 0; e < 16; e += 2) {
                     const int at = d + e;
                     const float2 v = Elem<T>::up(*(const uint32_t*)(values + l * 128 + at / 64 * Shape<D>::HALF_BYTES + ((at % 64 / 8) ^ (l & 7)) * 16 + at % 8 * 2));
                     if (seen) {
@@ -477,7 +480,7 @@ __device__ __noinline__ void add_lines(const uint32_t* lines, const uint8_t* val
                     }
                 }
                 __syncwarp();
-                bw_st32(O0 + d, x);
+                bw_st16(O0 + d, x);
                 bw_wait_st();
             }
         }
@@ -562,22 +565,19 @@ __device__ __noinline__ bool border_tile(const AttendArgs& a, Rest* s, Border& b
         float mx = -INFINITY;
         bool sees = false;                                        // a line without numbers
 #pragma unroll 1
-        for (int c = 0; c < TILE; c += 64) {
-            uint32_t x[64];
+        for (int c = 0; c < TILE; c += 32) {
+            uint32_t x[32];
             bw_ld32(b.S0 + c, x);
-            bw_ld32(b.S0 + c + 32, x + 32);
-            const uint32_t words[2] = {see.word(b.place + c), see.word(b.place + c + 32)};
-            sees |= (words[0] & s->lines[b.w][c / 32]) | (words[1] & s->lines[b.w][c / 32 + 1]);
+            const uint32_t word = see.word(b.place + c);
+            sees |= (word & s->lines[b.w][c / 32]) != 0;
             __syncwarp();
             bw_wait_ld32(x);
-            bw_wait_ld32(x + 32);
 #pragma unroll
-            for (int e = 0; e < 64; ++e) {
-                x[e] = words[e / 32] >> e % 32 & 1 ? x[e] : 0xFF800000u;
+            for (int e = 0; e < 32; ++e) {
+                x[e] = word >> e & 1 ? x[e] : 0xFF800000u;
                 mx = fmaxf(mx, __uint_as_float(x[e]));
             }
             bw_st32(b.S0 + c, x);
-            bw_st32(b.S0 + c + 32, x + 32);
         }
         bw_wait_st();
         if (lines && (b.first || __any_sync(~0u, sees))) {        // (the reference by the rule of whole tiles: what nobody sees changes no bit)
@@ -628,6 +628,7 @@ __device__ bool Softmax<T, D>::run(int n) {
     for (int j = w; j < jobs; j += 2) {
         const int k = k0 + (wide ? j >> 1 : j), number = k < sink_tiles ? k : k + behind;
         const bool masked = number >= plain_end || (number < plain_from && number >= sinks_end);
+        if (wide && j == 0 && (masked || !busy)) bw_arrive_warp(bw_smem(&s->lead));     // (a border takes both groups)
         if (masked) {
             const uint32_t vs = it + 2 * (wide ? j >> 1 : j) + 1;
             Border b = {base + S::RING + vs % S::SLOTS * S::SLOT_BYTES, S0, O0, bw_smem(&s->s_full[w]), s_count & 1, bw_smem(&s->full[vs % S::SLOTS]), (vs / S::SLOTS) & 1,
@@ -639,22 +640,27 @@ __device__ bool Softmax<T, D>::run(int n) {
             bw_fence_after();
         }
         ++s_count;
-        uint32_t x[TILE];
-        float power = 0.f;
         if (busy) {
+            // 32 scores at a time, the next ones on their way; twice from tensor memory, for the maximum and for the weights (all in registers at once: spills, and
+            // twice the instructions, which do not stay in the instruction cache)
+            uint32_t x[32], y[32];
+            float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            auto most = [&](const uint32_t* v) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) bw_ld32(S0 + 32 * c, x + 32 * c);
+                for (int e = 0; e < 32; e += 8)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) bw_wait_ld32(x + 32 * c);
-            float m[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) m[q] = __uint_as_float(x[q]);
-#pragma unroll
-            for (int e = 4; e + 8 <= TILE; e += 8)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) m[q] = max3(m[q], __uint_as_float(x[e + q]), __uint_as_float(x[e + 4 + q]));
-#pragma unroll
-            for (int q = 0; q < 4; ++q) m[q] = fmaxf(m[q], __uint_as_float(x[TILE - 4 + q]));
+                    for (int q = 0; q < 4; ++q) m[q] = max3(m[q], __uint_as_float(v[e + q]), __uint_as_float(v[e + 4 + q]));
+            };
+            bw_ld32(S0, x);
+#pragma unroll 1
+            for (int c = 0; c < TILE; c += 64) {
+                bw_wait_ld32(x);
+                bw_ld32(S0 + c + 32, y);
+                most(x);
+                bw_wait_ld32(y);
+                bw_ld32(S0 + (c + 64) % TILE, x);                 // (at the end: the first ones again)
+                most(y);
+            }
             const float mx = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
             const bool up = mx != -INFINITY && !((mx - top) * scale <= RESCALE);
             if (__any_sync(~0u, up)) {
@@ -663,20 +669,30 @@ __device__ bool Softmax<T, D>::run(int n) {
                 sum *= alpha;
                 if (j >= 2) scale_results<D>(O0, alpha);
             }
-            power = (top == -INFINITY ? 0.f : top * scale) - BIAS;
-        }
-        if (busy) {
+            const float power = (top == -INFINITY ? 0.f : top * scale) - BIAS;
+            if (wide && j == 0 && !masked) bw_arrive_warp(bw_smem(&s->lead));
             const float2 by = make_float2(scale, scale), less = make_float2(-power, -power);
             float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            auto weigh = [&](uint32_t* v) {
 #pragma unroll
-            for (int e = 0; e < TILE; e += 2) {
-                const float2 z = sd_fma2(make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), by, less);
-                const float2 p = make_float2(ex2(z.x), ex2(z.y));
-                part[e / 2 % 2] = sd_add2(part[e / 2 % 2], p);
-                x[e / 2] = weights<T>(p);
-                if (e == TILE / 2 - 2) bw_st32(S0, x);
+                for (int e = 0; e < 32; e += 2) {
+                    const float2 z = sd_fma2(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), by, less);
+                    const float2 p = make_float2(ex2(z.x), ex2(z.y));
+                    part[e / 2 % 2] = sd_add2(part[e / 2 % 2], p);
+                    v[e / 2] = weights<T>(p);
+                }
+            };
+#pragma unroll 1
+            for (int c = 0; c < TILE; c += 64) {                  // (weights are half as wide: they come to lie over scores that have been read)
+                bw_wait_ld32(x);
+                bw_ld32(S0 + c + 32, y);
+                weigh(x);
+                bw_st16(S0 + c / 2, x);
+                bw_wait_ld32(y);
+                if (c == 0) bw_ld32(S0 + 64, x);
+                weigh(y);
+                bw_st16(S0 + c / 2 + 16, y);
             }
-            bw_st32(S0 + 32, x + 32);
             sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
         }
         bw_wait_st();
@@ -764,16 +780,17 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
     using S = Shape<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
     Rest* s = (Rest*)(smem + S::REST);
-    const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+    const int t = threadIdx.x, warp = uniform(t >> 5), lane = t & 31;
     if (t == 0) {
-        for (int e = 0; e < S::SLOTS; ++e) { bw_bar_init(bw_smem(&s->full[e]), 1); bw_bar_init(bw_smem(&s->empty[e]), 1); }
+        for (int e = 0; e < S::SLOTS; ++e) { bw_bar_init(bw_smem(&s->full[e]), 1); bw_bar_init(bw_smem(&s->empty[e]), 2); }
         for (int e = 0; e < 2; ++e) {
             bw_bar_init(bw_smem(&s->s_full[e]), 1); bw_bar_init(bw_smem(&s->p_ready[e]), 4); bw_bar_init(bw_smem(&s->o_done[e]), 1);
-            bw_bar_init(bw_smem(&s->q_full[e]), 1); bw_bar_init(bw_smem(&s->q_empty[e]), 1); bw_bar_init(bw_smem(&s->group_meet[e]), 4);
+            bw_bar_init(bw_smem(&s->q_full[e]), 1); bw_bar_init(bw_smem(&s->q_empty[e]), 2); bw_bar_init(bw_smem(&s->group_meet[e]), 4);
+            bw_bar_init(bw_smem(&s->over[e]), 1);
         }
         for (int e = 0; e < UNITS; ++e) { bw_bar_init(bw_smem(&s->unit_full[e]), 1); bw_bar_init(bw_smem(&s->unit_empty[e]), 11); }
         bw_bar_init(bw_smem(&s->meet), 8);
-        bw_bar_init(bw_smem(&s->over), 1);
+        bw_bar_init(bw_smem(&s->lead), 4);
         s->stop = 0; s->begun[0] = s->begun[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -785,15 +802,15 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
     sd_chain_begin();
     const uint32_t tmem = s->tmem, ring = bw_smem(smem + S::RING), q = bw_smem(smem + S::Q);
     if (warp == 0) copy_lines<D>(a, &mk, &mv, s, ring, lane);
-    else if (warp == 1) {
-        if (lane == 0 && !multiply<T, D>(a, s, ring, q, tmem)) {
+    else if (warp == 1 || warp == 3) {
+        const int w = warp >> 1;
+        if (!multiply<T, D>(a, s, ring, q, tmem, w)) {
             int never = 0;                                        // the products in flight come to their end
-            bw_commit(bw_smem(&s->over));
-            bw_wait_slow(bw_smem(&s->over), 0, &never, 200000000ll);
+            bw_commit(bw_smem(&s->over[w]), lane == 0);
+            bw_wait_slow(bw_smem(&s->over[w]), 0, &never, 200000000ll);
         }
-    } else if (warp == 2) walk_units(a, s, lane);
-    else if (warp == 3) {
-        copy_queries<D>(a, &mq, s, q, lane);
+    } else if (warp == 2) {
+        walk_units<D>(a, &mq, s, q, lane);
         if (a.b.d_status) write_status(a, lane);
     } else {
         const int row = (t - 128) & 127;

@@ -126,14 +126,22 @@ __device__ __forceinline__ uint64_t bw_desc_across(uint32_t addr, uint32_t next)
 __device__ __forceinline__ constexpr uint32_t bw_idesc(bool bf16, int M, int N, bool b_across, bool minus_a = false) {
     return 1u << 4 | (minus_a ? 1u << 13 : 0u) | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (b_across ? 1u << 16 : 0u) | (uint32_t)(N >> 3) << 17 | (uint32_t)(M >> 4) << 24;
 }
-__device__ __forceinline__ void bw_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+// Called by a whole warp that stays together (so that operands are computed once for it); `leader`: one of its lanes, which issues.
+__device__ __forceinline__ void bw_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add, bool leader) {
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "r"((uint32_t)leader) : "memory");
 }
 // A from tensor memory: two elements a column.
-__device__ __forceinline__ void bw_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+__device__ __forceinline__ void bw_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add, bool leader) {
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "r"((uint32_t)leader) : "memory");
 }
-// The barrier is arrived at when all products that this thread has issued are done.
-__device__ __forceinline__ void bw_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+// The barrier is arrived at when all products that the leader has issued are done.
+__device__ __forceinline__ void bw_commit(uint32_t bar, bool leader) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"((uint32_t)leader) : "memory");
+}
+__device__ __forceinline__ bool bw_elect() {
+    uint32_t is;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+    return is;
 }
