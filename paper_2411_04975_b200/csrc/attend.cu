@@ -22,6 +22,7 @@ namespace {
 constexpr int TILE = 128;                                         // lines of the cache a step
 constexpr int THREADS = 384;                                      // four warps that feed, eight that compute
 constexpr int UNITS = 3;                                          // units that are known: the one at work and two more
+constexpr int CHUNKS = 64;                                        // that the requests are added up in
 constexpr int LEAST = 4;                                          // of a block's piece: a shorter one costs more to join than it saves
 constexpr float BIAS_FP16 = 7.0f;                                 // fp16 weights are 2^7 as large: more of the small ones are above its least number
 constexpr float RESCALE = 8.0f;                                   // results are rescaled when a row's maximum has grown by 2^8 (weights stay below that)
@@ -96,6 +97,7 @@ struct Rest {                     // of shared memory
     int stop;
     int begun[2];                 // the group has begun its results itself: the first product adds to them
     uint32_t lines[2][4];         // lines of the group's tile with values that are no numbers
+    int costs[CHUNKS], all, some; // of the list: chunks of requests, the whole; a request with rows (the prefix is read through its pages)
     Unit units[UNITS];
     float2 sums[2][128];          // of the groups' rows: reference and sum
 };
@@ -177,27 +179,37 @@ __device__ __noinline__ Quote quote_of(const AttendArgs& a, int prefix_tiles, in
     return e;
 }
 
+__device__ __forceinline__ int chunk_size(int n) { return (n + 32 * CHUNKS - 1) / (32 * CHUNKS) * 32; }
+
+// By the whole block: what the requests cost, in chunks.
+__device__ void add_up(const AttendArgs& a, Rest* s, int t) {
+    const int prefix_tiles = a.p.window ? 0 : a.p.shared / TILE, size = chunk_size(a.b.n);
+#pragma unroll 1
+    for (int first = t & ~31; first < a.b.n; first += THREADS) {  // (a warp's requests are in one chunk)
+        const int i = first + (t & 31);
+        int cost = 0, has = 0x7FFFFFFF;
+        if (i < a.b.n) {
+            const Quote e = quote_of(a, prefix_tiles, i);
+            cost = e.cost;
+            if (e.count) has = i;
+        }
+        __syncwarp();
+        cost = __reduce_add_sync(~0u, cost);
+        has = __reduce_min_sync(~0u, has);
+        if ((t & 31) == 0 && cost) {
+            atomicAdd(&s->costs[first / size], cost);
+            atomicAdd(&s->all, cost);
+            atomicMin(&s->some, has);
+        }
+    }
+}
+
 template <int D>
 __device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, uint32_t q, int lane) {
     using S = Shape<D>;
     const sd_rows& b = a.b;
     const int H = a.c.kv_heads, most = 2 * a.tile_rows;           // rows of a unit
-    const int prefix_tiles = a.p.window ? 0 : a.p.shared / TILE;
-    int sum = 0, some = 0x7FFFFFFF;                               // a request with rows: the prefix is read through its pages
-    Quote mine = {0, 0, 0, 0, 0, 0, 0};                           // of the first 32 requests
-#pragma unroll 1
-    for (int i = lane; i < b.n; i += 32) {
-        const Quote e = quote_of(a, prefix_tiles, i);
-        if (i == lane) mine = e;
-        sum += e.cost;
-        if (e.count) some = min(some, i);
-    }
-    __syncwarp();
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        sum += __shfl_xor_sync(~0u, sum, d);
-        some = min(some, __shfl_xor_sync(~0u, some, d));
-    }
+    const int prefix_tiles = a.p.window ? 0 : a.p.shared / TILE, sum = s->all, some = s->some;
     // the prefix, as if it were a request before the others, with all rows
     Quote prefix = {0, 0, a.p.shared, 0, 0, prefix_tiles, 0};
     if (prefix_tiles && sum) {
@@ -210,14 +222,27 @@ __device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, 
     Cut cut;
     cut.first = 0; cut.last = -1;
     int at = 0, base = 0;                                         // units handed out; of the list, what is behind
+    int start = prefix.cost ? -32 : 0;
+    if (lo >= prefix.cost) {                                      // the chunk of requests that the piece begins in
+        const int c0 = s->costs[2 * lane], c1 = s->costs[2 * lane + 1];
+        int end = c0 + c1;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int x = __shfl_up_sync(~0u, end, d);
+            if (lane >= d) end += x;
+        }
+        const int from = lo - prefix.cost, l = min(31, __popc(__ballot_sync(~0u, end <= from)));
+        const int before = __shfl_sync(~0u, end - c0 - c1, l), c = __shfl_sync(~0u, c0, l), second = before + c <= from;
+        start = (2 * l + second) * chunk_size(b.n);
+        base = prefix.cost + before + (second ? c : 0);
+    }
     uint32_t qi = 0;                                              // tiles of queries
     bool ok = true;
     // 32 requests at a time, then those of them that the piece touches, then their units
 #pragma unroll 1
-    for (int first = prefix.cost ? -32 : 0; ok && first < b.n && base < hi; first += 32) {
+    for (int first = start; ok && first < b.n && base < hi; first += 32) {
         Quote e = {0, 0, 0, 0, 0, 0, 0};
         if (first < 0) { if (lane == 0) e = prefix; }
-        else if (first == 0) e = mine;
         else if (first + lane < b.n) e = quote_of(a, prefix_tiles, first + lane);
         __syncwarp();
         int end = e.cost;
@@ -323,21 +348,19 @@ __device__ void copy_lines(const AttendArgs& a, const CUtensorMap* mk, const CUt
         const int length = kind == PREFIX ? v.cached : v.cached + v.count;
         bw_arrive_warp(bw_smem(&s->unit_empty[n % UNITS]));
         if (kind == DONE) return;
-        auto place_of = [&](int k) { return TILE * (k < sink_tiles ? k : next_tile + k - sink_tiles) + in_tile; };
-        auto page_of = [&](int k) {
-            const int p = place_of(k);
-            if (k >= k1 || in_tile >= TILE || p >= length) return -1;
-            const int page = sd_page(a.b, a.c.n_pages, request, p / P);
-            return page < 0 ? a.c.n_pages : page;                 // (a page that is none: beyond the last, where a copy fills in zeros)
-        };
-        int page = page_of(k0);
         bool ok = true;
+        int page = -1, line = 0;
 #pragma unroll 1
-        for (int k = k0; k < k1 && ok; ++k) {
-            const int next = page_of(k + 1), line = place_of(k) % P;
+        for (int k = k0 - 1; k < k1 && ok; ++k) {                 // (pages are looked up a tile ahead)
+            const int p = TILE * (k + 1 < sink_tiles ? k + 1 : next_tile + k + 1 - sink_tiles) + in_tile, entry = p / P;
+            int next = -1;
+            if (k + 1 < k1 && in_tile < TILE && p < length) {
+                next = sd_page(a.b, a.c.n_pages, request, entry);
+                if (next < 0) next = a.c.n_pages;                 // (a page that is none: beyond the last, where a copy fills in zeros)
+            }
             const int boxes = __popc(__ballot_sync(~0u, page >= 0));
 #pragma unroll 1
-            for (int v = 0; v < 2; ++v) {
+            for (int v = 0; v < 2 && k >= k0; ++v) {
                 const uint32_t e = it % S::SLOTS, bar = bw_smem(&s->full[e]);
                 ok = it < S::SLOTS || bw_wait_warp(bw_smem(&s->empty[e]), (it / S::SLOTS - 1) & 1, &s->stop);
                 if (!ok) break;
@@ -350,6 +373,7 @@ __device__ void copy_lines(const AttendArgs& a, const CUtensorMap* mk, const CUt
                 ++it;
             }
             page = next;
+            line = p - entry * P;
         }
         if (!ok) break;
     }
@@ -435,56 +459,12 @@ template <class T, int D>
 __device__ __forceinline__ uint32_t lines_without_numbers(const uint8_t* values, int t) {
     const uint8_t* mine = values + t * 128;
     uint32_t found = 0;
-#pragma unroll 4
+#pragma unroll 2
     for (int c = 0; c < D / 8; ++c) {
         const uint4 x = *(const uint4*)(mine + c / 8 * Shape<D>::HALF_BYTES + ((c % 8) ^ (t & 7)) * 16);
         found |= no_number<T>(x.x) | no_number<T>(x.y) | no_number<T>(x.z) | no_number<T>(x.w);
     }
     return __ballot_sync(~0u, found != 0);
-}
-
-// S0, O0: the warp's scores and results.  first: the results begin here.
-template <class T, int D>
-__device__ __noinline__ void add_lines(const uint32_t* lines, const uint8_t* values, uint32_t S0, uint32_t O0, bool first, const Sight& see, int place, float scale, float power) {
-    if (first)
-#pragma unroll 1
-        for (int c = 0; c < D; c += 16) {
-            uint32_t x[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = 0;
-            bw_st16(O0 + c, x);
-        }
-    bw_wait_st();
-#pragma unroll 1
-    for (int c = 0; c < 4; ++c) {
-        const uint32_t word = see.word(place + 32 * c);
-        __syncwarp();
-#pragma unroll 1
-        for (uint32_t left = lines[c]; left; left &= left - 1) {
-            const int l = 32 * c + __ffs(left) - 1;
-            const bool seen = word >> (l & 31) & 1;
-            if (!__any_sync(~0u, seen)) continue;
-            const float p = ex2(fmaf(__uint_as_float(bw_ld1(S0 + l)), scale, -power));
-#pragma unroll 1
-            for (int d = 0; d < D; d += 16) {
-                uint32_t x[16];
-                bw_ld16(O0 + d, x);
-                bw_wait_ld16(x);
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const int at = d + e;
-                    const float2 v = Elem<T>::up(*(const uint32_t*)(values + l * 128 + at / 64 * Shape<D>::HALF_BYTES + ((at % 64 / 8) ^ (l & 7)) * 16 + at % 8 * 2));
-                    if (seen) {
-                        x[e] = __float_as_uint(__uint_as_float(x[e]) + p * v.x);
-                        x[e + 1] = __float_as_uint(__uint_as_float(x[e + 1]) + p * v.y);
-                    }
-                }
-                __syncwarp();
-                bw_st16(O0 + d, x);
-                bw_wait_st();
-            }
-        }
-    }
 }
 
 // ---- softmax -------------------------------------------------------------------------------
@@ -533,8 +513,65 @@ __device__ __noinline__ void scale_results(uint32_t O0, float alpha) {
     bw_wait_st();
 }
 
-// A tile that not every row sees whole.  Scores that a row does not see become -inf, in tensor memory, so that the rest is the same for all tiles; and if lines of the
-// values hold no numbers, the row's reference is brought up to date, their part is added to the results and they are cleared (see above).
+// A tile's scores of a warp's rows become weights: 32 scores at a time, the next ones on their way; twice from tensor memory, for the maximum and for the
+// weights (all in registers at once: spills, and twice the instructions, which then do not stay in the instruction cache).
+// lead: a barrier to arrive at halfway, if any.
+template <class T, int D>
+__device__ __forceinline__ void weigh_tile(uint32_t S0, uint32_t O0, bool first, float scale, float& top, float& sum, uint32_t lead) {
+    uint32_t x[32], y[32];
+    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    auto most = [&](const uint32_t* v) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 8)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) m[q] = max3(m[q], __uint_as_float(v[e + q]), __uint_as_float(v[e + 4 + q]));
+    };
+    bw_ld32(S0, x);
+#pragma unroll 1
+    for (int c = 0; c < TILE; c += 64) {
+        bw_wait_ld32(x);
+        bw_ld32(S0 + c + 32, y);
+        most(x);
+        bw_wait_ld32(y);
+        bw_ld32(S0 + (c + 64) % TILE, x);                         // (at the end: the first ones again)
+        most(y);
+    }
+    const float mx = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+    const bool up = mx != -INFINITY && !((mx - top) * scale <= RESCALE);
+    if (__any_sync(~0u, up)) {
+        const float alpha = up ? ex2((top - mx) * scale) : 1.f;
+        if (up) top = mx;
+        sum *= alpha;
+        if (!first) scale_results<D>(O0, alpha);
+    }
+    if (lead) bw_arrive_warp(lead);
+    const float power = (top == -INFINITY ? 0.f : top * scale) - (IsBf16<T>::v ? 0.0f : BIAS_FP16);
+    const float2 by = make_float2(scale, scale), less = make_float2(-power, -power);
+    float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    auto weigh = [&](uint32_t* v) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+            const float2 z = sd_fma2(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), by, less);
+            const float2 p = make_float2(ex2(z.x), ex2(z.y));
+            part[e / 2 % 2] = sd_add2(part[e / 2 % 2], p);
+            v[e / 2] = weights<T>(p);
+        }
+    };
+#pragma unroll 1
+    for (int c = 0; c < TILE; c += 64) {                          // (weights are half as wide: they come to lie over scores that have been read)
+        bw_wait_ld32(x);
+        bw_ld32(S0 + c + 32, y);
+        weigh(x);
+        bw_st16(S0 + c / 2, x);
+        bw_wait_ld32(y);
+        if (c == 0) bw_ld32(S0 + 64, x);
+        weigh(y);
+        bw_st16(S0 + c / 2 + 16, y);
+    }
+    sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
+}
+
+// A tile that not every row sees whole.  Scores that a row does not see become -inf, in tensor memory, so that the rest is the same for all tiles.  If lines of its values hold no numbers, those that the warp's rows see are added to the results and all are cleared (see above).
 // Out of line: in the loop over tiles its instructions and registers cost whole tiles a quarter of their time.
 struct Border {
     uint8_t* values;
@@ -545,6 +582,58 @@ struct Border {
     float top, sum;
 };
 
+// What the warp's rows see of lines without numbers, added to their results (which begin here if it is the first tile).  The rows' reference is brought up to this tile
+// before, by the rule of all tiles: lines that nobody sees change no bit.
+template <class T, int D>
+__device__ __noinline__ void add_lines(const uint32_t* lines, Border& b, float scale) {
+    float mx = -INFINITY;
+#pragma unroll 1
+    for (int c = 0; c < TILE; ++c) {
+        mx = fmaxf(mx, __uint_as_float(bw_ld1(b.S0 + c)));
+    }
+    const bool up = mx != -INFINITY && !((mx - b.top) * scale <= RESCALE);
+    const float alpha = up ? ex2((b.top - mx) * scale) : 1.f;
+    if (up) b.top = mx;
+    b.sum *= alpha;
+    __syncwarp();
+    if (!b.first) scale_results<D>(b.O0, alpha);
+    else
+#pragma unroll 1
+        for (int c = 0; c < D; c += 16) {
+            uint32_t x[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = 0;
+            bw_st16(b.O0 + c, x);
+        }
+    bw_wait_st();
+    const float power = (b.top == -INFINITY ? 0.f : b.top * scale) - (IsBf16<T>::v ? 0.0f : BIAS_FP16);
+#pragma unroll 1
+    for (int l = 0; l < TILE; ++l) {
+        if (!(lines[l / 32] >> l % 32 & 1)) continue;
+        const bool seen = b.see.word(b.place + l) & 1;
+        if (!__any_sync(~0u, seen)) continue;
+        const float p = ex2(fmaf(__uint_as_float(bw_ld1(b.S0 + l)), scale, -power));
+#pragma unroll 1
+        for (int d = 0; d < D; d += 16) {
+            uint32_t x[16];
+            bw_ld16(b.O0 + d, x);
+            bw_wait_ld16(x);
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                const int at = d + e;
+                const float2 v = Elem<T>::up(*(const uint32_t*)(b.values + l * 128 + at / 64 * Shape<D>::HALF_BYTES + ((at % 64 / 8) ^ (l & 7)) * 16 + at % 8 * 2));
+                if (seen) {
+                    x[e] = __float_as_uint(__uint_as_float(x[e]) + p * v.x);
+                    x[e + 1] = __float_as_uint(__uint_as_float(x[e + 1]) + p * v.y);
+                }
+            }
+            __syncwarp();
+            bw_st16(b.O0 + d, x);
+            bw_wait_st();
+        }
+    }
+}
+
 template <class T, int D>
 __device__ __noinline__ bool border_tile(const AttendArgs& a, Rest* s, Border& b) {
     using S = Shape<D>;
@@ -553,7 +642,6 @@ __device__ __noinline__ bool border_tile(const AttendArgs& a, Rest* s, Border& b
         bw_arrive_warp(bar);
         return bw_wait_warp(bar, parity, &s->stop);
     };
-    const Sight see = b.see;
     if (!bw_wait_warp(b.v_full, b.v_parity, &s->stop)) return false;
     const uint32_t of_warp = lines_without_numbers<T, D>(b.values, b.t);
     if ((b.t & 31) == 0) s->lines[b.w][b.t >> 5] = of_warp;
@@ -562,34 +650,21 @@ __device__ __noinline__ bool border_tile(const AttendArgs& a, Rest* s, Border& b
     if (!bw_wait_warp(b.s_full, b.s_parity, &s->stop)) return false;
     bw_fence_after();
     if (b.busy) {
-        float mx = -INFINITY;
-        bool sees = false;                                        // a line without numbers
+        bool seen = false;
 #pragma unroll 1
         for (int c = 0; c < TILE; c += 32) {
             uint32_t x[32];
             bw_ld32(b.S0 + c, x);
-            const uint32_t word = see.word(b.place + c);
-            sees |= (word & s->lines[b.w][c / 32]) != 0;
+            const uint32_t word = b.see.word(b.place + c);
+            seen |= (word & s->lines[b.w][c / 32]) != 0;
             __syncwarp();
             bw_wait_ld32(x);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-                x[e] = word >> e & 1 ? x[e] : 0xFF800000u;
-                mx = fmaxf(mx, __uint_as_float(x[e]));
-            }
+            for (int e = 0; e < 32; ++e) x[e] = word >> e & 1 ? x[e] : 0xFF800000u;
             bw_st32(b.S0 + c, x);
         }
         bw_wait_st();
-        if (lines && (b.first || __any_sync(~0u, sees))) {        // (the reference by the rule of whole tiles: what nobody sees changes no bit)
-            const bool up = mx != -INFINITY && !((mx - b.top) * a.scale <= RESCALE);
-            const float alpha = up ? ex2((b.top - mx) * a.scale) : 1.f;
-            if (up) b.top = mx;
-            b.sum *= alpha;
-            __syncwarp();
-            if (!b.first) scale_results<D>(b.O0, alpha);
-            const float power = (b.top == -INFINITY ? 0.f : b.top * a.scale) - (IsBf16<T>::v ? 0.0f : BIAS_FP16);
-            add_lines<T, D>(s->lines[b.w], b.values, b.S0, b.O0, b.first, see, b.place, a.scale, power);
-        }
+        if (lines && (b.first || __any_sync(~0u, seen))) add_lines<T, D>(s->lines[b.w], b, a.scale);
     }
     if (!lines) return true;
     if (b.first && b.t == 0) s->begun[b.w] = 1;
@@ -600,6 +675,7 @@ __device__ __noinline__ bool border_tile(const AttendArgs& a, Rest* s, Border& b
         bw_fence_async();
     }
     __syncwarp();
+    b.first = false;                                              // (results have begun)
     return b.both ? meet(true) : true;
 }
 
@@ -629,72 +705,19 @@ __device__ bool Softmax<T, D>::run(int n) {
         const int k = k0 + (wide ? j >> 1 : j), number = k < sink_tiles ? k : k + behind;
         const bool masked = number >= plain_end || (number < plain_from && number >= sinks_end);
         if (wide && j == 0 && (masked || !busy)) bw_arrive_warp(bw_smem(&s->lead));     // (a border takes both groups)
+        bool begins = j < 2;                                      // the group's results
         if (masked) {
             const uint32_t vs = it + 2 * (wide ? j >> 1 : j) + 1;
             Border b = {base + S::RING + vs % S::SLOTS * S::SLOT_BYTES, S0, O0, bw_smem(&s->s_full[w]), s_count & 1, bw_smem(&s->full[vs % S::SLOTS]), (vs / S::SLOTS) & 1,
                         meets, group_meets, see, w, t, number * TILE, busy, j < 2, wide, top, sum};
             if (!border_tile<T, D>(a, s, b)) return false;
-            meets = b.meets; group_meets = b.group_meets; top = b.top; sum = b.sum;
+            meets = b.meets; group_meets = b.group_meets; top = b.top; sum = b.sum; begins = b.first;
         } else {
             if (!bw_wait_warp(bw_smem(&s->s_full[w]), s_count & 1, &s->stop)) return false;
             bw_fence_after();
         }
         ++s_count;
-        if (busy) {
-            // 32 scores at a time, the next ones on their way; twice from tensor memory, for the maximum and for the weights (all in registers at once: spills, and
-            // twice the instructions, which do not stay in the instruction cache)
-            uint32_t x[32], y[32];
-            float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            auto most = [&](const uint32_t* v) {
-#pragma unroll
-                for (int e = 0; e < 32; e += 8)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) m[q] = max3(m[q], __uint_as_float(v[e + q]), __uint_as_float(v[e + 4 + q]));
-            };
-            bw_ld32(S0, x);
-#pragma unroll 1
-            for (int c = 0; c < TILE; c += 64) {
-                bw_wait_ld32(x);
-                bw_ld32(S0 + c + 32, y);
-                most(x);
-                bw_wait_ld32(y);
-                bw_ld32(S0 + (c + 64) % TILE, x);                 // (at the end: the first ones again)
-                most(y);
-            }
-            const float mx = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-            const bool up = mx != -INFINITY && !((mx - top) * scale <= RESCALE);
-            if (__any_sync(~0u, up)) {
-                const float alpha = up ? ex2((top - mx) * scale) : 1.f;
-                if (up) top = mx;
-                sum *= alpha;
-                if (j >= 2) scale_results<D>(O0, alpha);
-            }
-            const float power = (top == -INFINITY ? 0.f : top * scale) - BIAS;
-            if (wide && j == 0 && !masked) bw_arrive_warp(bw_smem(&s->lead));
-            const float2 by = make_float2(scale, scale), less = make_float2(-power, -power);
-            float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-            auto weigh = [&](uint32_t* v) {
-#pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    const float2 z = sd_fma2(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), by, less);
-                    const float2 p = make_float2(ex2(z.x), ex2(z.y));
-                    part[e / 2 % 2] = sd_add2(part[e / 2 % 2], p);
-                    v[e / 2] = weights<T>(p);
-                }
-            };
-#pragma unroll 1
-            for (int c = 0; c < TILE; c += 64) {                  // (weights are half as wide: they come to lie over scores that have been read)
-                bw_wait_ld32(x);
-                bw_ld32(S0 + c + 32, y);
-                weigh(x);
-                bw_st16(S0 + c / 2, x);
-                bw_wait_ld32(y);
-                if (c == 0) bw_ld32(S0 + 64, x);
-                weigh(y);
-                bw_st16(S0 + c / 2 + 16, y);
-            }
-            sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
-        }
+        if (busy) weigh_tile<T, D>(S0, O0, begins, scale, top, sum, wide && j == 0 && !masked ? bw_smem(&s->lead) : 0);
         bw_wait_st();
         bw_fence_before();
         bw_arrive_warp(bw_smem(&s->p_ready[w]));
@@ -741,25 +764,23 @@ __device__ __forceinline__ bool Softmax<T, D>::finish(const Unit& u, float top, 
     T* out = (T*)a.out + (u.begin + r) * a.p.out_stride[0] + h * a.p.out_stride[1];
     float* part = to == SLOT ? a.part + ((long long)u.slot * 256 + mrow) * D : a.plane[u.slot & 1] + at * D;
 #pragma unroll 1
-    for (int c = c0; c < c1; c += 16) {
-        uint32_t x[16], z[16];
-        bw_ld16(A + c, x);
-        if (two) bw_ld16(A + TILE + c, z);
-        bw_wait_ld16(x);
-        if (two) bw_wait_ld16(z);
-        float y[16];
+    for (int c = c0; c < c1; c += 8) {
+        uint32_t x[8], z[8];
+        bw_ld8(A + c, x);
+        if (two) bw_ld8(A + TILE + c, z);
+        bw_wait_ld8(x);
+        if (two) bw_wait_ld8(z);
+        float y[8];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {                            // (a part without a weight may hold anything)
+        for (int e = 0; e < 8; ++e) {                             // (a part without a weight may hold anything)
             y[e] = g0 == 0.f ? 0.f : __uint_as_float(x[e]) * g0;
-            if (two && g1 != 0.f) y[e] += __uint_as_float(z[e]) * g1;
+            if (g1 != 0.f) y[e] += __uint_as_float(z[e]) * g1;
         }
         if (row) {
-            if (to == FINAL) {
-                *(uint4*)(out + c) = sd_pack<T>(y);
-                *(uint4*)(out + c + 8) = sd_pack<T>(y + 8);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 16; e += 4) *(float4*)(part + c + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+            if (to == FINAL) *(uint4*)(out + c) = sd_pack<T>(y);
+            else {
+                *(float4*)(part + c) = make_float4(y[0], y[1], y[2], y[3]);
+                *(float4*)(part + c + 4) = make_float4(y[4], y[5], y[6], y[7]);
             }
         }
         __syncwarp();
@@ -794,12 +815,16 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
         s->stop = 0; s->begun[0] = s->begun[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (t < CHUNKS) s->costs[t] = 0;
+    if (t == CHUNKS) { s->all = 0; s->some = 0x7FFFFFFF; }
     if (t == 32 * 3) { bw_prefetch_map(&mk); bw_prefetch_map(&mv); bw_prefetch_map(&mq); }
     if (warp == 1) bw_tmem_alloc(bw_smem(&s->tmem), 512);
     bw_fence_before();
     __syncthreads();
     bw_fence_after();
-    sd_chain_begin();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    add_up(a, s, t);
+    __syncthreads();
     const uint32_t tmem = s->tmem, ring = bw_smem(smem + S::RING), q = bw_smem(smem + S::Q);
     if (warp == 0) copy_lines<D>(a, &mk, &mv, s, ring, lane);
     else if (warp == 1 || warp == 3) {
@@ -823,6 +848,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
     __syncwarp();
     bw_fence_before();
     __syncthreads();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (from the begin on, the next kernel's waiting blocks cost small calls a quarter)
     if (warp == 1) {
         bw_fence_after();
         bw_tmem_free(tmem, 512);
@@ -833,7 +859,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
 
 // ---- joining -------------------------------------------------------------------------------
 // A warp per packed row of a cut unit: its parts by their sums.
-constexpr int JOIN_ROWS = 8;
+constexpr int JOIN_ROWS = 8, MOST_BLOCKS = 1024;
 
 template <class T, int D>
 __device__ void join_row(const AttendArgs& a, const Cut& c, int m, int lane, bool planes) {
@@ -858,7 +884,7 @@ __device__ void join_row(const AttendArgs& a, const Cut& c, int m, int lane, boo
         top = most;
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] *= keep;
-#pragma unroll 8
+#pragma unroll 4
         for (int k = 0; k < n; ++k) {
             const float* y = a.part + slot(first + k) * D + lane * E;
             const float g = __shfl_sync(~0u, f, k);
@@ -889,12 +915,38 @@ __device__ void join_row(const AttendArgs& a, const Cut& c, int m, int lane, boo
 }
 
 template <class T, int D>
-__global__ void __launch_bounds__(32 * JOIN_ROWS) join_cuts_kernel(const __grid_constant__ AttendArgs a, bool planes) {
+__global__ void __launch_bounds__(32 * JOIN_ROWS) join_cuts_kernel(const __grid_constant__ AttendArgs a, bool planes, int blocks) {
     sd_chain_begin();
-    const Cut c = a.cuts[blockIdx.x];
-    if (c.last < c.first) return;
-    const int lane = threadIdx.x & 31, packed = c.rows * a.group;
-    for (int m = blockIdx.y * JOIN_ROWS + (threadIdx.x >> 5); m < packed; m += gridDim.y * JOIN_ROWS) join_row<T, D>(a, c, m, lane, planes);
+    __shared__ int s_end[MOST_BLOCKS], s_warp[JOIN_ROWS];         // packed rows of the cuts up to each
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    int base = 0;
+    for (int first = 0; first < blocks; first += 32 * JOIN_ROWS) {
+        int rows = 0;
+        if (first + t < blocks) {
+            const Cut c = a.cuts[first + t];
+            if (c.last >= c.first) rows = c.rows * a.group;
+        }
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int x = __shfl_up_sync(~0u, rows, d);
+            if (lane >= d) rows += x;
+        }
+        if (lane == 31) s_warp[warp] = rows;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) rows += s_warp[w];
+        if (first + t < blocks) s_end[first + t] = base + rows;
+        __syncthreads();
+        base = s_end[min(first + 32 * JOIN_ROWS, blocks) - 1];
+    }
+    for (int m = blockIdx.x * JOIN_ROWS + warp; m < base; m += gridDim.x * JOIN_ROWS) {
+        int lo = 0, hi = blocks - 1;                              // the first cut that ends behind m
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (s_end[mid] > m) hi = mid;
+            else lo = mid + 1;
+        }
+        join_row<T, D>(a, a.cuts[lo], m - (lo ? s_end[lo - 1] : 0), lane, planes);
+    }
 }
 
 // With a shared prefix: it and what is behind it, a warp per row and head.
@@ -963,7 +1015,7 @@ int room_for(const sd_cache* c, const sd_rows* b, const sd_attend_params* p, Roo
     const long long units = c->kv_heads * 2 * (b->n + (b->rows + most - 1) / most);
     if (units > (1ll << 31) / (longest + 1)) return SD_ERR_CAPACITY;
     r->planes = p->shared >= TILE && !p->window;
-    r->blocks = (int)std::max(1ll, std::min((long long)sms, (units * (longest + 1) + LEAST - 1) / LEAST));
+    r->blocks = (int)std::max(1ll, std::min((long long)std::min(sms, MOST_BLOCKS), (units * (longest + 1) + LEAST - 1) / LEAST));
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t was = at; at += (bytes + 255) / 256 * 256; return was; };
     r->cuts = take(r->blocks * (int64_t)sizeof(Cut));
@@ -1020,13 +1072,9 @@ int launch(const AttendArgs& a, const Room& r, cudaStream_t st) {
     SD_CUDA_OK(cudaFuncSetAttribute(attend_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D>()));
     SD_CUDA_OK(sd_launch(attend_kernel<T, D>, r.blocks, THREADS, smem_bytes<D>(), st, a, mk, mv, mq));
     if (a.b.rows == 0) return SD_OK;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(r.blocks, std::min((std::min(a.b.max_draft + 1, 2 * a.tile_rows) * a.group + JOIN_ROWS - 1) / JOIN_ROWS, 16)); cfg.blockDim = dim3(32 * JOIN_ROWS); cfg.stream = st;
-    cfg.attrs = &attr; cfg.numAttrs = 1;
-    SD_CUDA_OK(cudaLaunchKernelEx(&cfg, join_cuts_kernel<T, D>, a, r.planes));
+    // (Blocks for the rows that there can be, or four a multiprocessor.)
+    const long long rows = std::min((long long)a.b.rows * a.p.q_heads, (long long)r.blocks * 2 * a.tile_rows * a.group);
+    SD_CUDA_OK(sd_launch(join_cuts_kernel<T, D>, (unsigned)std::min((rows + JOIN_ROWS - 1) / JOIN_ROWS, 4ll * r.blocks), 32 * JOIN_ROWS, 0, st, a, r.planes, r.blocks));
     if (r.planes) SD_CUDA_OK(sd_launch(join_planes_kernel<T, D>, a.b.rows, 256, 0, st, a));
     return SD_OK;
 }

@@ -34,16 +34,19 @@ __device__ __noinline__ bool bw_wait_slow(uint32_t bar, uint32_t parity, volatil
     }
     return true;
 }
-__device__ __forceinline__ bool bw_wait(uint32_t bar, uint32_t parity, volatile int* stop) {
-    if (bw_try(bar, parity)) return true;
-    return bw_wait_slow(bar, parity, stop, 4000000000ll);
-}
 // ... for a whole warp: all of its lanes go on or none does.  They come together first: lanes that wait may keep the others of their warp from running, so none of them may
 // still have something to do that the barrier waits for.
+__device__ __noinline__ bool bw_wait_slow_warp(uint32_t bar, uint32_t parity, volatile int* stop) {
+    const long long begin = clock64();
+    while (!__all_sync(~0u, bw_try(bar, parity))) {
+        if (__any_sync(~0u, *stop || clock64() - begin > 4000000000ll)) { *stop = 1; return false; }
+    }
+    return true;
+}
 __device__ __forceinline__ bool bw_wait_warp(uint32_t bar, uint32_t parity, volatile int* stop) {
     __syncwarp();
-    const bool ok = bw_wait(bar, parity, stop);
-    return __all_sync(~0u, ok);
+    if (__all_sync(~0u, bw_try(bar, parity))) return true;
+    return bw_wait_slow_warp(bar, parity, stop);
 }
 
 __device__ __forceinline__ void bw_fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }   // plain writes before what the tensor cores and copies do
@@ -97,6 +100,13 @@ __device__ __forceinline__ void bw_wait_ld16(uint32_t* r) {
 __device__ __forceinline__ void bw_st16(uint32_t at, const uint32_t* r) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
                  ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(at) : "memory");
+}
+__device__ __forceinline__ void bw_ld8(uint32_t at, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(at));
+}
+__device__ __forceinline__ void bw_wait_ld8(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])::"memory");
 }
 __device__ __forceinline__ uint32_t bw_ld1(uint32_t at) {
     uint32_t x;
