@@ -513,130 +513,83 @@ __device__ __noinline__ void scale_results(uint32_t O0, float alpha) {
     bw_wait_st();
 }
 
-// A tile's scores of a warp's rows become weights: 32 scores at a time, the next ones on their way; twice from tensor memory, for the maximum and for the
-// weights (all in registers at once: spills, and twice the instructions, which then do not stay in the instruction cache).
-// lead: a barrier to arrive at halfway, if any.
-template <class T, int D>
-__device__ __forceinline__ void weigh_tile(uint32_t S0, uint32_t O0, bool first, float scale, float& top, float& sum, uint32_t lead) {
-    uint32_t x[32], y[32];
-    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    auto most = [&](const uint32_t* v) {
+// The largest of 32 scores and m.
+__device__ __forceinline__ void most_of(const uint32_t* v, float* m) {
 #pragma unroll
-        for (int e = 0; e < 32; e += 8)
+    for (int e = 0; e < 32; e += 8)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) m[q] = max3(m[q], __uint_as_float(v[e + q]), __uint_as_float(v[e + 4 + q]));
-    };
-    bw_ld32(S0, x);
-#pragma unroll 1
-    for (int c = 0; c < TILE; c += 64) {
-        bw_wait_ld32(x);
-        bw_ld32(S0 + c + 32, y);
-        most(x);
-        bw_wait_ld32(y);
-        bw_ld32(S0 + (c + 64) % TILE, x);                         // (at the end: the first ones again)
-        most(y);
-    }
-    const float mx = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-    const bool up = mx != -INFINITY && !((mx - top) * scale <= RESCALE);
-    if (__any_sync(~0u, up)) {
-        const float alpha = up ? ex2((top - mx) * scale) : 1.f;
-        if (up) top = mx;
-        sum *= alpha;
-        if (!first) scale_results<D>(O0, alpha);
-    }
-    if (lead) bw_arrive_warp(lead);
-    const float power = (top == -INFINITY ? 0.f : top * scale) - (IsBf16<T>::v ? 0.0f : BIAS_FP16);
-    const float2 by = make_float2(scale, scale), less = make_float2(-power, -power);
-    float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-    auto weigh = [&](uint32_t* v) {
-#pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-            const float2 z = sd_fma2(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), by, less);
-            const float2 p = make_float2(ex2(z.x), ex2(z.y));
-            part[e / 2 % 2] = sd_add2(part[e / 2 % 2], p);
-            v[e / 2] = weights<T>(p);
-        }
-    };
-#pragma unroll 1
-    for (int c = 0; c < TILE; c += 64) {                          // (weights are half as wide: they come to lie over scores that have been read)
-        bw_wait_ld32(x);
-        bw_ld32(S0 + c + 32, y);
-        weigh(x);
-        bw_st16(S0 + c / 2, x);
-        bw_wait_ld32(y);
-        if (c == 0) bw_ld32(S0 + 64, x);
-        weigh(y);
-        bw_st16(S0 + c / 2 + 16, y);
-    }
-    sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
+        for (int q = 0; q < 4; ++q) m[q] = max3(m[q], __uint_as_float(v[e + q]), __uint_as_float(v[e + 4 + q]));
 }
 
-// A tile that not every row sees whole.  Scores that a row does not see become -inf, in tensor memory, so that the rest is the same for all tiles.  If lines of its values hold no numbers, those that the warp's rows see are added to the results and all are cleared (see above).
-// Out of line: in the loop over tiles its instructions and registers cost whole tiles a quarter of their time.
+// A tile that not every row sees whole: scores that a row does not see become -inf, in tensor memory, so that the rest is the same for all tiles.  Returns the largest.
+// (Out of line, as all that follows for such tiles: in the loop over tiles its instructions and registers cost whole tiles a quarter of their time.)
+__device__ __noinline__ float hide(const Sight& see, int place, uint32_t S0) {
+    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+    for (int c = 0; c < TILE; c += 32) {
+        uint32_t x[32];
+        bw_ld32(S0 + c, x);
+        const uint32_t word = see.word(place + c);
+        const bool whole = __all_sync(~0u, word == ~0u);
+        bw_wait_ld32(x);
+        if (!whole) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) x[e] = word >> e & 1 ? x[e] : 0xFF800000u;
+            bw_st32(S0 + c, x);
+        }
+        most_of(x, m);
+    }
+    bw_wait_st();
+    return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+}
+
+// Behind the weights of such a tile: if lines of its values hold no numbers, those that the warp's rows see are added to the results and all are cleared (see above).
 struct Border {
     uint8_t* values;
-    uint32_t S0, O0, s_full, s_parity, v_full, v_parity, meets, group_meets;
-    Sight see;
+    uint32_t S0, O0, v_full, v_parity, meets, group_meets;
     int w, t, place;
     bool busy, first, both;
-    float top, sum;
 };
 
-// What the warp's rows see of lines without numbers, added to their results (which begin here if it is the first tile).  The rows' reference is brought up to this tile
-// before, by the rule of all tiles: lines that nobody sees change no bit.
+// Their part in the results, which begin here if it is the first tile.
 template <class T, int D>
-__device__ __noinline__ void add_lines(const uint32_t* lines, Border& b, float scale) {
-    float mx = -INFINITY;
+__device__ __noinline__ void add_lines(const uint32_t* lines, const Sight& see, const Border& b) {
+    if (b.first)
 #pragma unroll 1
-    for (int c = 0; c < TILE; ++c) {
-        mx = fmaxf(mx, __uint_as_float(bw_ld1(b.S0 + c)));
-    }
-    const bool up = mx != -INFINITY && !((mx - b.top) * scale <= RESCALE);
-    const float alpha = up ? ex2((b.top - mx) * scale) : 1.f;
-    if (up) b.top = mx;
-    b.sum *= alpha;
-    __syncwarp();
-    if (!b.first) scale_results<D>(b.O0, alpha);
-    else
-#pragma unroll 1
-        for (int c = 0; c < D; c += 16) {
-            uint32_t x[16];
+        for (int c = 0; c < D; c += 8) {
+            uint32_t x[8];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = 0;
-            bw_st16(b.O0 + c, x);
+            for (int e = 0; e < 8; ++e) x[e] = 0;
+            bw_st8(b.O0 + c, x);
         }
     bw_wait_st();
-    const float power = (b.top == -INFINITY ? 0.f : b.top * scale) - (IsBf16<T>::v ? 0.0f : BIAS_FP16);
 #pragma unroll 1
     for (int l = 0; l < TILE; ++l) {
         if (!(lines[l / 32] >> l % 32 & 1)) continue;
-        const bool seen = b.see.word(b.place + l) & 1;
+        const bool seen = see.word(b.place + l) & 1;
         if (!__any_sync(~0u, seen)) continue;
-        const float p = ex2(fmaf(__uint_as_float(bw_ld1(b.S0 + l)), scale, -power));
+        const uint32_t two = bw_ld1(b.S0 + l / 2);
+        const float2 weight = Elem<T>::up(two);
+        const float p = l % 2 ? weight.y : weight.x;
 #pragma unroll 1
-        for (int d = 0; d < D; d += 16) {
-            uint32_t x[16];
-            bw_ld16(b.O0 + d, x);
-            bw_wait_ld16(x);
+        for (int d = 0; d < D; d += 8) {
+            uint32_t x[8];
+            bw_ld8(b.O0 + d, x);
+            bw_wait_ld8(x);
+            float v[8];
+            sd_unpack<T>(*(const uint4*)(b.values + l * 128 + d / 64 * Shape<D>::HALF_BYTES + ((d % 64 / 8) ^ (l & 7)) * 16), v);
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-                const int at = d + e;
-                const float2 v = Elem<T>::up(*(const uint32_t*)(b.values + l * 128 + at / 64 * Shape<D>::HALF_BYTES + ((at % 64 / 8) ^ (l & 7)) * 16 + at % 8 * 2));
-                if (seen) {
-                    x[e] = __float_as_uint(__uint_as_float(x[e]) + p * v.x);
-                    x[e + 1] = __float_as_uint(__uint_as_float(x[e + 1]) + p * v.y);
-                }
-            }
+            for (int e = 0; e < 8; ++e)
+                if (seen) x[e] = __float_as_uint(__uint_as_float(x[e]) + p * v[e]);
             __syncwarp();
-            bw_st16(b.O0 + d, x);
+            bw_st8(b.O0 + d, x);
             bw_wait_st();
         }
     }
 }
 
 template <class T, int D>
-__device__ __noinline__ bool border_tile(const AttendArgs& a, Rest* s, Border& b) {
-    using S = Shape<D>;
+__device__ __noinline__ bool clear_lines(Rest* s, const Sight& see, Border& b) {
     auto meet = [&](bool both) {
         const uint32_t bar = bw_smem(both ? &s->meet : &s->group_meet[b.w]), parity = (both ? b.meets++ : b.group_meets++) & 1;
         bw_arrive_warp(bar);
@@ -646,36 +599,19 @@ __device__ __noinline__ bool border_tile(const AttendArgs& a, Rest* s, Border& b
     const uint32_t of_warp = lines_without_numbers<T, D>(b.values, b.t);
     if ((b.t & 31) == 0) s->lines[b.w][b.t >> 5] = of_warp;
     if (!meet(b.both)) return false;
-    const uint32_t lines = s->lines[b.w][0] | s->lines[b.w][1] | s->lines[b.w][2] | s->lines[b.w][3];
-    if (!bw_wait_warp(b.s_full, b.s_parity, &s->stop)) return false;
-    bw_fence_after();
-    if (b.busy) {
-        bool seen = false;
-#pragma unroll 1
-        for (int c = 0; c < TILE; c += 32) {
-            uint32_t x[32];
-            bw_ld32(b.S0 + c, x);
-            const uint32_t word = b.see.word(b.place + c);
-            seen |= (word & s->lines[b.w][c / 32]) != 0;
-            __syncwarp();
-            bw_wait_ld32(x);
+    uint32_t lines = 0;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = word >> e & 1 ? x[e] : 0xFF800000u;
-            bw_st32(b.S0 + c, x);
-        }
-        bw_wait_st();
-        if (lines && (b.first || __any_sync(~0u, seen))) add_lines<T, D>(s->lines[b.w], b, a.scale);
-    }
+    for (int c = 0; c < 4; ++c) lines |= s->lines[b.w][c];
     if (!lines) return true;
+    if (b.busy) add_lines<T, D>(s->lines[b.w], see, b);
     if (b.first && b.t == 0) s->begun[b.w] = 1;
     if (!meet(b.both)) return false;
     if ((s->lines[b.w][b.t >> 5] >> (b.t & 31) & 1) && (b.w == 0 || !b.both)) {
 #pragma unroll 1
-        for (int c = 0; c < D / 8; ++c) *(uint4*)(b.values + b.t * 128 + c / 8 * S::HALF_BYTES + c % 8 * 16) = make_uint4(0, 0, 0, 0);
+        for (int c = 0; c < D / 8; ++c) *(uint4*)(b.values + b.t * 128 + c / 8 * Shape<D>::HALF_BYTES + c % 8 * 16) = make_uint4(0, 0, 0, 0);
         bw_fence_async();
     }
     __syncwarp();
-    b.first = false;                                              // (results have begun)
     return b.both ? meet(true) : true;
 }
 
@@ -705,19 +641,74 @@ __device__ bool Softmax<T, D>::run(int n) {
         const int k = k0 + (wide ? j >> 1 : j), number = k < sink_tiles ? k : k + behind;
         const bool masked = number >= plain_end || (number < plain_from && number >= sinks_end);
         if (wide && j == 0 && (masked || !busy)) bw_arrive_warp(bw_smem(&s->lead));     // (a border takes both groups)
-        bool begins = j < 2;                                      // the group's results
-        if (masked) {
-            const uint32_t vs = it + 2 * (wide ? j >> 1 : j) + 1;
-            Border b = {base + S::RING + vs % S::SLOTS * S::SLOT_BYTES, S0, O0, bw_smem(&s->s_full[w]), s_count & 1, bw_smem(&s->full[vs % S::SLOTS]), (vs / S::SLOTS) & 1,
-                        meets, group_meets, see, w, t, number * TILE, busy, j < 2, wide, top, sum};
-            if (!border_tile<T, D>(a, s, b)) return false;
-            meets = b.meets; group_meets = b.group_meets; top = b.top; sum = b.sum; begins = b.first;
-        } else {
-            if (!bw_wait_warp(bw_smem(&s->s_full[w]), s_count & 1, &s->stop)) return false;
-            bw_fence_after();
+        if (!bw_wait_warp(bw_smem(&s->s_full[w]), s_count++ & 1, &s->stop)) return false;
+        bw_fence_after();
+        if (busy) {
+            // 32 scores at a time, the next ones on their way; twice from tensor memory, for the maximum and for the weights (all in registers at once: spills, and
+            // twice the instructions, which then do not stay in the instruction cache)
+            uint32_t x[32], y[32];
+            float mx;
+            if (masked) {
+                mx = hide(see, number * TILE, S0);
+                bw_ld32(S0, x);
+            } else {
+                float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                bw_ld32(S0, x);
+#pragma unroll 1
+                for (int c = 0; c < TILE; c += 64) {
+                    bw_wait_ld32(x);
+                    bw_ld32(S0 + c + 32, y);
+                    most_of(x, m);
+                    bw_wait_ld32(y);
+                    bw_ld32(S0 + (c + 64) % TILE, x);             // (at the end: the first ones again)
+                    most_of(y, m);
+                }
+                mx = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+            }
+            const bool up = mx != -INFINITY && !((mx - top) * scale <= RESCALE);
+            if (__any_sync(~0u, up)) {
+                const float alpha = up ? ex2((top - mx) * scale) : 1.f;
+                if (up) top = mx;
+                sum *= alpha;
+                if (j >= 2) {
+                    bw_wait_ld32(x);
+                    scale_results<D>(O0, alpha);
+                    bw_ld32(S0, x);
+                }
+            }
+            if (wide && j == 0 && !masked) bw_arrive_warp(bw_smem(&s->lead));
+            const float power = (top == -INFINITY ? 0.f : top * scale) - BIAS;
+            const float2 by = make_float2(scale, scale), less = make_float2(-power, -power);
+            float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            auto weigh = [&](uint32_t* v) {
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    const float2 z = sd_fma2(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), by, less);
+                    const float2 p = make_float2(ex2(z.x), ex2(z.y));
+                    part[e / 2 % 2] = sd_add2(part[e / 2 % 2], p);
+                    v[e / 2] = weights<T>(p);
+                }
+            };
+#pragma unroll 1
+            for (int c = 0; c < TILE; c += 64) {                  // (weights are half as wide: they come to lie over scores that have been read)
+                bw_wait_ld32(x);
+                bw_ld32(S0 + c + 32, y);
+                weigh(x);
+                bw_st16(S0 + c / 2, x);
+                bw_wait_ld32(y);
+                if (c == 0) bw_ld32(S0 + 64, x);
+                weigh(y);
+                bw_st16(S0 + c / 2 + 16, y);
+            }
+            sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
         }
-        ++s_count;
-        if (busy) weigh_tile<T, D>(S0, O0, begins, scale, top, sum, wide && j == 0 && !masked ? bw_smem(&s->lead) : 0);
+        if (masked) {
+            bw_wait_st();
+            const uint32_t vs = it + 2 * (wide ? j >> 1 : j) + 1;
+            Border b = {base + S::RING + vs % S::SLOTS * S::SLOT_BYTES, S0, O0, bw_smem(&s->full[vs % S::SLOTS]), (vs / S::SLOTS) & 1, meets, group_meets, w, t, number * TILE, busy, j < 2, wide};
+            if (!clear_lines<T, D>(s, see, b)) return false;
+            meets = b.meets; group_meets = b.group_meets;
+        }
         bw_wait_st();
         bw_fence_before();
         bw_arrive_warp(bw_smem(&s->p_ready[w]));
@@ -764,23 +755,25 @@ __device__ __forceinline__ bool Softmax<T, D>::finish(const Unit& u, float top, 
     T* out = (T*)a.out + (u.begin + r) * a.p.out_stride[0] + h * a.p.out_stride[1];
     float* part = to == SLOT ? a.part + ((long long)u.slot * 256 + mrow) * D : a.plane[u.slot & 1] + at * D;
 #pragma unroll 1
-    for (int c = c0; c < c1; c += 8) {
-        uint32_t x[8], z[8];
-        bw_ld8(A + c, x);
-        if (two) bw_ld8(A + TILE + c, z);
-        bw_wait_ld8(x);
-        if (two) bw_wait_ld8(z);
-        float y[8];
+    for (int c = c0; c < c1; c += 16) {
+        uint32_t x[16], z[16];
+        bw_ld16(A + c, x);
+        if (two) bw_ld16(A + TILE + c, z);
+        bw_wait_ld16(x);
+        if (two) bw_wait_ld16(z);
+        float y[16];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {                             // (a part without a weight may hold anything)
+        for (int e = 0; e < 16; ++e) {                            // (a part without a weight may hold anything)
             y[e] = g0 == 0.f ? 0.f : __uint_as_float(x[e]) * g0;
             if (g1 != 0.f) y[e] += __uint_as_float(z[e]) * g1;
         }
         if (row) {
-            if (to == FINAL) *(uint4*)(out + c) = sd_pack<T>(y);
-            else {
-                *(float4*)(part + c) = make_float4(y[0], y[1], y[2], y[3]);
-                *(float4*)(part + c + 4) = make_float4(y[4], y[5], y[6], y[7]);
+            if (to == FINAL) {
+                *(uint4*)(out + c) = sd_pack<T>(y);
+                *(uint4*)(out + c + 8) = sd_pack<T>(y + 8);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) *(float4*)(part + c + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
             }
         }
         __syncwarp();
