@@ -6,7 +6,7 @@
 // falls so, so that every multiprocessor reads as much of the cache as any other, whatever the lengths; each block finds its piece from the lengths by itself.
 // Rows of a unit that was cut are left as partial results (normalised, with the logarithm of their sum) and joined by a second kernel.
 //
-// A block is a warp that copies keys and values into a ring in shared memory, one that walks the list and copies queries, and two groups of four warps that
+// A block is a warp that walks the list and copies queries and keys, one that copies values, both into a ring in shared memory, and two groups of four warps that
 // compute the softmax, a thread per packed row, each with a warp that issues its products.  Two chains of (scores, softmax, product with the values)
 // are in flight, one per group: for a unit of up to 128 rows the groups take tiles in turns and join their results at the end, for a larger one each has 128 rows of every tile.
 // While one group is at its softmax the tensor cores work for the other.  Scores and results are in tensor memory; the weights go back over the scores
@@ -160,6 +160,75 @@ __device__ __noinline__ void drain(uint64_t* full, uint32_t slots, uint32_t fill
     }
 }
 
+// ---- copies --------------------------------------------------------------------------------
+// A unit's keys (v = 0) or values (1): slots of the ring in turns.  (A warp for each: a copy takes 75 to 90 cycles to issue, and a tile of small pages is many.)
+template <int D>
+struct Lines {
+    using S = Shape<D>;
+    const AttendArgs& a;
+    const CUtensorMap* map;
+    Rest* s;
+    const uint32_t ring, v;
+    const int piece, half;                                        // of a tile and of a head, that this lane fetches
+    uint32_t it;                                                  // the next slot
+    // what is known of the tile to come
+    bool here;
+    int page, line;
+
+    // Pages are looked up a tile ahead, and not looked at before they are needed.  Lines that no row sees are not fetched.
+    __device__ __forceinline__ void look(const Unit& u, int k) {
+        const int in_tile = piece * a.box, p = TILE * (k < u.sink_tiles ? k : u.next_tile + k - u.sink_tiles) + in_tile, entry = p / a.c.page_size;
+        const int W = a.p.window, from = W && u.kind == TAIL ? max(0, u.cached - W + 1) : 0, length = u.kind == PREFIX ? u.cached : u.cached + u.count;
+        here = k < u.k1 && in_tile < TILE && p < length && (p + a.box > from || (p < a.p.sinks && p < u.cached));
+        page = 0;
+        if (here) page = a.b.d_table[(long long)u.request * a.b.table_stride + entry];
+        line = p - entry * a.c.page_size;
+    }
+    // Tile k of the unit, whose pages have been looked up, and a look at the next.  False: given up.
+    __device__ __forceinline__ bool copy(const Unit& u, int k, bool wide) {
+        const uint32_t e = it % S::SLOTS, bar = bw_smem(&s->full[e]);
+        const int boxes = __popc(__ballot_sync(~0u, here));
+        if (it >= S::SLOTS && !bw_wait_warp(bw_smem(&s->empty[e]), (it / S::SLOTS - 1) & 1, &s->stop)) return false;
+        if ((threadIdx.x & 31) == 0) {
+            if (!wide) bw_arrive(bw_smem(&s->empty[e]));          // (for the group that does not use it)
+            bw_arrive_expect(bar, boxes * a.box * 128);
+        }
+        if ((unsigned)page >= (unsigned)a.c.n_pages) page = a.c.n_pages;                  // (a page that is none: beyond the last, where a copy fills in zeros)
+        const bool was = here;
+        const int y = line, w = page;
+        look(u, k + 1);
+        __syncwarp();
+        if (was) bw_load_4d(ring + e * S::SLOT_BYTES + half * S::HALF_BYTES + piece * a.box * 128, map, half * 64, y, u.head, w, bar);
+        it += 2;
+        return true;
+    }
+    // Given up: this warp's copies in flight come to their end.
+    __device__ __noinline__ void drain() {
+        for (uint32_t k = it >= 2 * S::SLOTS ? it - 2 * S::SLOTS : v; k < it; k += 2) {
+            int never = 0;
+            bw_wait_slow(bw_smem(&s->full[k % S::SLOTS]), (k / S::SLOTS) & 1, &never, 200000000ll);
+        }
+    }
+};
+
+template <int D>
+__device__ void copy_values(Lines<D> f) {
+    for (int n = 0;; ++n) {
+        if (!bw_wait_warp(bw_smem(&f.s->unit_full[n % UNITS]), (n / UNITS) & 1, &f.s->stop)) break;
+        const Unit& u = f.s->units[n % UNITS];
+        if (u.kind == DONE) return;
+        const bool wide = u.rows > f.a.tile_rows;
+        const int k1 = u.k1;
+        bool ok = true;
+        f.look(u, u.k0);
+#pragma unroll 1
+        for (int k = u.k0; k < k1 && ok; ++k) ok = f.copy(u, k, wide);
+        if (!ok) break;
+        bw_arrive_warp(bw_smem(&f.s->unit_empty[n % UNITS]));
+    }
+    f.drain();
+}
+
 // ---- the list's walker ---------------------------------------------------------------------
 // What a request's units cost: their tiles, and one more each for a unit's begin and end.  (31 bits are enough: the host has seen to that.)
 struct Quote {
@@ -204,8 +273,9 @@ __device__ void add_up(const AttendArgs& a, Rest* s, int t) {
     }
 }
 
+// Hands out the units of the block's piece, and copies their queries and keys.
 template <int D>
-__device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, uint32_t q, int lane) {
+__device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, uint32_t q, Lines<D> keys, int lane) {
     using S = Shape<D>;
     const sd_rows& b = a.b;
     const int H = a.c.kv_heads, most = 2 * a.tile_rows;           // rows of a unit
@@ -288,14 +358,22 @@ __device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, 
                     bw_arrive(bw_smem(&s->unit_full[place]));
                 }
                 ++at;
-                // its queries: a tile's rows and heads in one copy for each half of the head; rows behind the unit's come along and are left alone
+                const bool wide = u.rows > a.tile_rows;
+                keys.look(u, u.k0);
 #pragma unroll 1
-                for (int row = 0; row < u.rows && ok; row += a.tile_rows, ++qi) {
-                    const uint32_t slot = qi % 2, bar = bw_smem(&s->q_full[slot]);
-                    ok = qi < 2 || bw_wait_warp(bw_smem(&s->q_empty[slot]), (qi / 2 - 1) & 1, &s->stop);
-                    if (!ok || lane) continue;
-                    bw_arrive_expect(bar, S::HALVES * 128 * a.group * a.tile_rows);
-                    for (int h = 0; h < S::HALVES; ++h) bw_load_3d(q + slot * S::Q_BYTES + h * S::HALF_BYTES, mq, h * 64, u.head * a.group, (int)u.begin + row, bar);
+                for (int k = u.k0; k < u.k1 && ok; ++k) {
+                    ok = keys.copy(u, k, wide);
+                    if (k > u.k0) continue;
+                    // its queries: a tile's rows and heads in one copy for each half of the head; rows behind the unit's come along and are left alone
+#pragma unroll 1
+                    for (int row = 0; row < u.rows && ok; row += a.tile_rows, ++qi) {
+                        const uint32_t slot = qi % 2, bar = bw_smem(&s->q_full[slot]);
+                        ok = qi < 2 || bw_wait_warp(bw_smem(&s->q_empty[slot]), (qi / 2 - 1) & 1, &s->stop);
+                        if (!ok || lane) continue;
+                        bw_arrive_expect(bar, S::HALVES * 128 * a.group * a.tile_rows);
+#pragma unroll 1
+                        for (int h = 0; h < S::HALVES; ++h) bw_load_3d(q + slot * S::Q_BYTES + h * S::HALF_BYTES, mq, h * 64, u.head * a.group, (int)u.begin + row, bar);
+                    }
                 }
                 if (!ok) break;
             }
@@ -308,7 +386,10 @@ __device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, 
         s->units[e].kind = DONE;
         bw_arrive(bw_smem(&s->unit_full[e]));
     }
-    if (!ok) drain(s->q_full, 2, qi);
+    if (!ok) {
+        drain(s->q_full, 2, qi);
+        keys.drain();
+    }
 }
 
 // Pages that a request's rows see: told where one is none of the cache's.
@@ -330,54 +411,6 @@ __device__ void write_status(const AttendArgs& a, int lane) {
         }
         if (lane == 0) b.d_status[i] = st;
     }
-}
-
-// ---- copies --------------------------------------------------------------------------------
-template <int D>
-__device__ void copy_lines(const AttendArgs& a, const CUtensorMap* mk, const CUtensorMap* mv, Rest* s, uint32_t ring, int lane) {
-    using S = Shape<D>;
-    const int P = a.c.page_size, box = a.box;
-    const int piece = lane / S::HALVES, half = lane % S::HALVES, in_tile = piece * box;
-    const uint32_t to = half * S::HALF_BYTES + in_tile * 128;
-    uint32_t it = 0;                                              // slots filled
-    for (int n = 0;; ++n) {
-        if (!bw_wait_warp(bw_smem(&s->unit_full[n % UNITS]), (n / UNITS) & 1, &s->stop)) break;
-        const Unit& v = s->units[n % UNITS];
-        const int kind = v.kind, request = v.request, head = v.head, k0 = v.k0, k1 = v.k1, sink_tiles = v.sink_tiles, next_tile = v.next_tile;
-        const bool wide = v.rows > a.tile_rows;
-        const int length = kind == PREFIX ? v.cached : v.cached + v.count;
-        bw_arrive_warp(bw_smem(&s->unit_empty[n % UNITS]));
-        if (kind == DONE) return;
-        bool ok = true;
-        int page = -1, line = 0;
-#pragma unroll 1
-        for (int k = k0 - 1; k < k1 && ok; ++k) {                 // (pages are looked up a tile ahead)
-            const int p = TILE * (k + 1 < sink_tiles ? k + 1 : next_tile + k + 1 - sink_tiles) + in_tile, entry = p / P;
-            int next = -1;
-            if (k + 1 < k1 && in_tile < TILE && p < length) {
-                next = sd_page(a.b, a.c.n_pages, request, entry);
-                if (next < 0) next = a.c.n_pages;                 // (a page that is none: beyond the last, where a copy fills in zeros)
-            }
-            const int boxes = __popc(__ballot_sync(~0u, page >= 0));
-#pragma unroll 1
-            for (int v = 0; v < 2 && k >= k0; ++v) {
-                const uint32_t e = it % S::SLOTS, bar = bw_smem(&s->full[e]);
-                ok = it < S::SLOTS || bw_wait_warp(bw_smem(&s->empty[e]), (it / S::SLOTS - 1) & 1, &s->stop);
-                if (!ok) break;
-                if (lane == 0) {
-                    if (!wide) bw_arrive(bw_smem(&s->empty[e]));  // (for the group that does not use it)
-                    bw_arrive_expect(bar, boxes * box * 128);
-                }
-                __syncwarp();
-                if (page >= 0) bw_load_4d(ring + e * S::SLOT_BYTES + to, v ? mv : mk, half * 64, line, head, page, bar);
-                ++it;
-            }
-            page = next;
-            line = p - entry * P;
-        }
-        if (!ok) break;
-    }
-    drain(s->full, S::SLOTS, it);
 }
 
 // ---- products ------------------------------------------------------------------------------
@@ -819,7 +852,14 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
     add_up(a, s, t);
     __syncthreads();
     const uint32_t tmem = s->tmem, ring = bw_smem(smem + S::RING), q = bw_smem(smem + S::Q);
-    if (warp == 0) copy_lines<D>(a, &mk, &mv, s, ring, lane);
+    if (warp == 0 || warp == 2) {
+        Lines<D> f = {a, warp ? &mv : &mk, s, ring, (uint32_t)warp >> 1, lane / S::HALVES, lane % S::HALVES, (uint32_t)warp >> 1};
+        if (warp == 0) walk_units<D>(a, &mq, s, q, f, lane);
+        else {
+            copy_values<D>(f);
+            if (a.b.d_status) write_status(a, lane);
+        }
+    }
     else if (warp == 1 || warp == 3) {
         const int w = warp >> 1;
         if (!multiply<T, D>(a, s, ring, q, tmem, w)) {
@@ -827,9 +867,6 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
             bw_commit(bw_smem(&s->over[w]), lane == 0);
             bw_wait_slow(bw_smem(&s->over[w]), 0, &never, 200000000ll);
         }
-    } else if (warp == 2) {
-        walk_units<D>(a, &mq, s, q, lane);
-        if (a.b.d_status) write_status(a, lane);
     } else {
         const int row = (t - 128) & 127;
         Softmax<T, D> f = {a, s, smem, tmem + ((uint32_t)(warp & 3) << 21), (warp - 4) >> 2, row, row / a.group, row % a.group};
