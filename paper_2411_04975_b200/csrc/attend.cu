@@ -23,7 +23,10 @@ constexpr int TILE = 128;                                         // lines of th
 constexpr int THREADS = 384;                                      // four warps that feed, eight that compute
 constexpr int UNITS = 3;                                          // units that are known: the one at work and two more
 constexpr int CHUNKS = 64;                                        // that the requests are added up in
-constexpr int LEAST = 4;                                          // of a block's piece: a shorter one costs more to join than it saves
+// What the list's parts cost (measured: a tile of one group's rows 2,000 cycles where the cache's bandwidth is not what holds it up, of both 3,800 at most; a unit's
+// begin and end 12,000).
+constexpr int NARROW = 2, WIDE = 3, ENDS = 8;
+constexpr int LEAST = 8;                                          // of a block's piece: a shorter one costs more to join than it saves
 constexpr float BIAS_FP16 = 7.0f;                                 // fp16 weights are 2^7 as large: more of the small ones are above its least number
 constexpr float RESCALE = 8.0f;                                   // results are rescaled when a row's maximum has grown by 2^8 (weights stay below that)
 
@@ -230,20 +233,27 @@ __device__ void copy_values(Lines<D> f) {
 }
 
 // ---- the list's walker ---------------------------------------------------------------------
-// What a request's units cost: their tiles, and one more each for a unit's begin and end.  (31 bits are enough: the host has seen to that.)
+// What a request's units cost.  (31 bits are enough: the host has seen to that.)
 struct Quote {
     long long begin;
     int count, cached;            // its rows, the places before them
     int sinks, next, tiles;       // of a unit
+    int last;                     // cost of a head's last unit (which may have less rows than the others)
     int cost;                     // of all
 };
+__device__ __forceinline__ int unit_cost(bool wide, int tiles) { return ENDS + tiles * (wide ? WIDE : NARROW); }
+__device__ __forceinline__ void price(Quote& e, int heads, int tile_rows) {
+    const int before = (e.count - 1) / (2 * tile_rows);           // units of a head before the last
+    e.last = unit_cost(e.count - before * 2 * tile_rows > tile_rows, e.tiles);
+    e.cost = heads * (before * unit_cost(true, e.tiles) + e.last);
+}
 __device__ __noinline__ Quote quote_of(const AttendArgs& a, int prefix_tiles, int i) {
     const Request r = sd_request(a.b, i, a.c.page_size, a.p.shared);
-    Quote e = {r.begin, r.count, r.cached, 0, 0, 0, 0};
+    Quote e = {r.begin, r.count, r.cached, 0, 0, 0, 0, 0};
     if (r.count) {
         const Tiles t = tiles_of(a.p, prefix_tiles, r);
         e.sinks = t.sinks; e.next = t.next; e.tiles = t.count;
-        e.cost = a.c.kv_heads * ((r.count + 2 * a.tile_rows - 1) / (2 * a.tile_rows)) * (t.count + 1);
+        price(e, a.c.kv_heads, a.tile_rows);
     }
     return e;
 }
@@ -281,11 +291,11 @@ __device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, 
     const int H = a.c.kv_heads, most = 2 * a.tile_rows;           // rows of a unit
     const int prefix_tiles = a.p.window ? 0 : a.p.shared / TILE, sum = s->all, some = s->some;
     // the prefix, as if it were a request before the others, with all rows
-    Quote prefix = {0, 0, a.p.shared, 0, 0, prefix_tiles, 0};
+    Quote prefix = {0, 0, a.p.shared, 0, 0, prefix_tiles, 0, 0};
     if (prefix_tiles && sum) {
         const long long rows = b.d_offsets[b.n];
         prefix.count = rows < 0 ? 0 : (int)min(rows, (long long)b.rows);
-        prefix.cost = H * ((prefix.count + most - 1) / most) * (prefix_tiles + 1);
+        if (prefix.count) price(prefix, H, a.tile_rows);
     }
     const int all = sum + prefix.cost, quota = max((all + (int)gridDim.x - 1) / (int)gridDim.x, LEAST);
     const int lo = (int)min((long long)quota * blockIdx.x, (long long)all), hi = min(lo + quota, all);
@@ -311,7 +321,7 @@ __device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, 
     // 32 requests at a time, then those of them that the piece touches, then their units
 #pragma unroll 1
     for (int first = start; ok && first < b.n && base < hi; first += 32) {
-        Quote e = {0, 0, 0, 0, 0, 0, 0};
+        Quote e = {0, 0, 0, 0, 0, 0, 0, 0};
         if (first < 0) { if (lane == 0) e = prefix; }
         else if (first + lane < b.n) e = quote_of(a, prefix_tiles, first + lane);
         __syncwarp();
@@ -332,22 +342,28 @@ __device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, 
             u.request = first < 0 ? some : first + l;
             u.cached = __shfl_sync(~0u, e.cached, l); u.count = __shfl_sync(~0u, e.count, l);
             u.sink_tiles = __shfl_sync(~0u, e.sinks, l); u.next_tile = __shfl_sync(~0u, first < 0 ? 0 : e.next, l);
-            const int begin = __shfl_sync(~0u, end - e.cost, l), tiles = __shfl_sync(~0u, e.tiles, l), per = tiles + 1, parts = (u.count + most - 1) / most;
+            const int begin = __shfl_sync(~0u, end - e.cost, l), tiles = __shfl_sync(~0u, e.tiles, l), last = __shfl_sync(~0u, e.last, l);
+            const int parts = (u.count + most - 1) / most, full = unit_cost(true, tiles), per_head = (parts - 1) * full + last;
             const long long rows_begin = __shfl_sync(~0u, e.begin, l);
-            int k = max(0, lo - begin) / per, head = k / parts, part = k - head * parts;
+            int off = max(0, lo - begin), head = off / per_head, part = min((off - head * per_head) / full, parts - 1);
+            int from = begin + head * per_head + part * full;
 #pragma unroll 1
-            for (int from = begin + k * per; from < hi && head < H; from += per) {
-                const int to = from + 1 + tiles;                  // its tiles are from + 1 ..
+            while (from < hi && head < H) {
                 u.head = head; u.row0 = part * most; u.begin = rows_begin + u.row0;
                 u.rows = min(most, u.count - u.row0);
-                u.k0 = max(from + 1, lo) - from - 1; u.k1 = min(to, hi) - from - 1;
+                const bool wide = u.rows > a.tile_rows;
+                // tile k begins at first + k * step of the list; the block that has this place has the tile
+                const int first_place = from + ENDS, step = wide ? WIDE : NARROW;
+                u.k0 = (max(lo - first_place, 0) + step - 1) / step;
+                u.k1 = min((max(hi - first_place, 0) + step - 1) / step, tiles);
+                from += part == parts - 1 ? last : full;
                 if (++part == parts) { part = 0; ++head; }
                 if (u.k1 <= u.k0) continue;
                 const bool whole = u.k0 == 0 && u.k1 == tiles;
                 u.to = !whole ? SLOT : prefix_tiles ? PLANE : FINAL;
                 u.slot = whole ? first < 0 : 2 * blockIdx.x + (u.k0 == 0);
                 if (!whole && u.k0 == 0) {
-                    cut.first = blockIdx.x; cut.last = (to - 1) / quota;
+                    cut.first = blockIdx.x; cut.last = (first_place + (tiles - 1) * step) / quota;
                     cut.rows = u.rows; cut.head = u.head; cut.prefix = first < 0; cut.begin = u.begin;
                 }
                 const int place = at % UNITS;
@@ -358,7 +374,6 @@ __device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, 
                     bw_arrive(bw_smem(&s->unit_full[place]));
                 }
                 ++at;
-                const bool wide = u.rows > a.tile_rows;
                 keys.look(u, u.k0);
 #pragma unroll 1
                 for (int k = u.k0; k < u.k1 && ok; ++k) {
@@ -492,7 +507,7 @@ template <class T, int D>
 __device__ __forceinline__ uint32_t lines_without_numbers(const uint8_t* values, int t) {
     const uint8_t* mine = values + t * 128;
     uint32_t found = 0;
-#pragma unroll 2
+#pragma unroll 4
     for (int c = 0; c < D / 8; ++c) {
         const uint4 x = *(const uint4*)(mine + c / 8 * Shape<D>::HALF_BYTES + ((c % 8) ^ (t & 7)) * 16);
         found |= no_number<T>(x.x) | no_number<T>(x.y) | no_number<T>(x.z) | no_number<T>(x.w);
@@ -558,19 +573,24 @@ __device__ __forceinline__ void most_of(const uint32_t* v, float* m) {
 // (Out of line, as all that follows for such tiles: in the loop over tiles its instructions and registers cost whole tiles a quarter of their time.)
 __device__ __noinline__ float hide(const Sight& see, int place, uint32_t S0) {
     float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-    for (int c = 0; c < TILE; c += 32) {
-        uint32_t x[32];
-        bw_ld32(S0 + c, x);
+    uint32_t x[32], y[32];
+    auto hidden = [&](uint32_t* v, int c) {
         const uint32_t word = see.word(place + c);
         const bool whole = __all_sync(~0u, word == ~0u);
-        bw_wait_ld32(x);
+        bw_wait_ld32(v);
+        if (c + 32 < TILE) bw_ld32(S0 + c + 32, v == x ? y : x);
         if (!whole) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = word >> e & 1 ? x[e] : 0xFF800000u;
-            bw_st32(S0 + c, x);
+            for (int e = 0; e < 32; ++e) v[e] = word >> e & 1 ? v[e] : 0xFF800000u;
+            bw_st32(S0 + c, v);
         }
-        most_of(x, m);
+        most_of(v, m);
+    };
+    bw_ld32(S0, x);
+#pragma unroll 1
+    for (int c = 0; c < TILE; c += 64) {
+        hidden(x, c);
+        hidden(y, c + 32);
     }
     bw_wait_st();
     return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
@@ -787,11 +807,11 @@ __device__ __forceinline__ bool Softmax<T, D>::finish(const Unit& u, float top, 
     const long long at = (u.begin + r) * a.p.q_heads + h;         // row and query head
     T* out = (T*)a.out + (u.begin + r) * a.p.out_stride[0] + h * a.p.out_stride[1];
     float* part = to == SLOT ? a.part + ((long long)u.slot * 256 + mrow) * D : a.plane[u.slot & 1] + at * D;
+    uint32_t x[16], z[16];
+    bw_ld16(A + c0, x);
+    if (two) bw_ld16(A + TILE + c0, z);
 #pragma unroll 1
     for (int c = c0; c < c1; c += 16) {
-        uint32_t x[16], z[16];
-        bw_ld16(A + c, x);
-        if (two) bw_ld16(A + TILE + c, z);
         bw_wait_ld16(x);
         if (two) bw_wait_ld16(z);
         float y[16];
@@ -799,6 +819,11 @@ __device__ __forceinline__ bool Softmax<T, D>::finish(const Unit& u, float top, 
         for (int e = 0; e < 16; ++e) {                            // (a part without a weight may hold anything)
             y[e] = g0 == 0.f ? 0.f : __uint_as_float(x[e]) * g0;
             if (g1 != 0.f) y[e] += __uint_as_float(z[e]) * g1;
+        }
+        __syncwarp();
+        if (c + 16 < c1) {                                        // (the next ones come while these are written)
+            bw_ld16(A + c + 16, x);
+            if (two) bw_ld16(A + TILE + c + 16, z);
         }
         if (row) {
             if (to == FINAL) {
@@ -1043,9 +1068,9 @@ int room_for(const sd_cache* c, const sd_rows* b, const sd_attend_params* p, Roo
     // all of the list, at the longest lengths that the tables hold
     const long long longest = ((long long)b->table_stride * c->page_size + TILE - 1) / TILE + 1, most = 2 * (128 / (p->q_heads / c->kv_heads));
     const long long units = c->kv_heads * 2 * (b->n + (b->rows + most - 1) / most);
-    if (units > (1ll << 31) / (longest + 1)) return SD_ERR_CAPACITY;
+    if (units > (1ll << 31) / (longest * WIDE + ENDS)) return SD_ERR_CAPACITY;
     r->planes = p->shared >= TILE && !p->window;
-    r->blocks = (int)std::max(1ll, std::min((long long)std::min(sms, MOST_BLOCKS), (units * (longest + 1) + LEAST - 1) / LEAST));
+    r->blocks = (int)std::max(1ll, std::min((long long)std::min(sms, MOST_BLOCKS), (units * (longest * WIDE + ENDS) + LEAST - 1) / LEAST));
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t was = at; at += (bytes + 255) / 256 * 256; return was; };
     r->cuts = take(r->blocks * (int64_t)sizeof(Cut));
