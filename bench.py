@@ -79,6 +79,8 @@ def parse():
                     help="scalability sweep over the size of the global tree (shape of the paper's appendix table)")
     ap.add_argument("--sweep-oracle", action="store_true",
                     help="with --sweep: time the CPU oracle beside every row (one thread, a sample of the requests)")
+    ap.add_argument("--verify", action="store_true",
+                    help="closed_loop config: a small attention model on the GPU verifies the drafts (sd_rotate, sd_attend, sd_accept, sd_commit)")
     ap.add_argument("--closed-loop-oracle", action="store_true",
                     help="closed_loop config: run the CPU oracle in lock-step and compare every step (slow)")
     return ap.parse_args()
@@ -548,7 +550,7 @@ def run_closed_loop(args):
     import torch
 
     import paper_2411_04975_b200 as sfx
-    from workload.closed_loop import ClosedLoop
+    from workload.closed_loop import ClosedLoop, accept_longest_path
 
     torch.cuda.set_device(0)
     dev = torch.device("cuda", 0)
@@ -567,6 +569,26 @@ def run_closed_loop(args):
     loop = ClosedLoop(w, B)
     slots_all = torch.arange(B, dtype=torch.int32, device=dev)
     out = store.alloc_outputs(B)
+    model, verify_ms, same = None, [], True
+    if args.verify:
+        from workload.verifier import Verifier
+        model = Verifier(B, c.prompt_len + c.out_len_hi + 8, c.max_spec, c.vocab, device=dev)
+
+    def verify():
+        """The drafts through the model on the GPU; tokens accepted per slot, to compare with the harness."""
+        last = torch.as_tensor(np.asarray([loop.last_token(s) for s in range(B)], dtype=np.int64), device=dev)
+        follows = np.full((B, c.max_spec + 1), -1, dtype=np.int64)
+        for s in range(B):
+            t = loop.truth[s][loop.cursor[s]:][:c.max_spec + 1]
+            follows[s, :len(t)] = t
+        follows = torch.as_tensor(follows, device=dev)
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        got = model.step(out, last, follows)
+        b.record()
+        lengths = got["offsets"].diff().cpu().numpy()
+        verify_ms.append(a.elapsed_time(b))
+        return lengths
 
     side = torch.cuda.Stream(device=dev)
 
@@ -634,7 +656,10 @@ def run_closed_loop(args):
         enqueue(prepare(items))
 
     refill_ev, kernel_ev = [], []
-    append(loop.start())
+    first = loop.start()
+    append(first)
+    if model:
+        model.start(first[0], first[1])
     torch.cuda.synchronize()
     refill_ev.clear()
     kernel_ev.clear()
@@ -657,7 +682,17 @@ def run_closed_loop(args):
             for n in ("n_draft", "tokens", "parents", "positions", "chosen_tree", "chosen_p"):
                 ok = ok and np.array_equal(g[n], r[n])
             ok = ok and np.array_equal(g["score"].view(np.int64), r["score"].view(np.int64))
-        prep = prepare(loop.advance(host))
+        if model:
+            lengths = verify()
+            want = [min(accept_longest_path(host["tokens"][s], host["parents"][s], int(host["n_draft"][s]), loop.truth[s][loop.cursor[s]:]) + 1,
+                        len(loop.truth[s]) - loop.cursor[s]) for s in range(B)]
+            left = [len(loop.truth[s]) - loop.cursor[s] for s in range(B)]
+            same = same and all(min(int(lengths[s]), left[s]) == want[s] for s in range(B))
+        items = loop.advance(host)
+        if model:
+            new = [i for i in range(len(items[0])) if items[0][i] >= 0 and items[2][i]]
+            model.start([items[0][i] for i in new], [items[1][i] for i in new])
+        prep = prepare(items)
         e1b = torch.cuda.Event(enable_timing=True)
         e1b.record()
         enqueue(prep)
@@ -696,6 +731,10 @@ def run_closed_loop(args):
                              "max_us": max(k_ms) * 1e3, "global_tokens_per_call": statistics.mean(g_tok),
                              "us_per_global_token": sum(k_ms) * 1e3 / max(sum(g_tok), 1)}
     line.update(summ)
+    if model:
+        v = verify_ms[Wc:]
+        line["verify"] = {"model": f"{model.layers} layers, {model.q_heads} query and {model.kv_heads} key heads of {model.head}", "mean_ms": statistics.mean(v),
+                          "p50_ms": statistics.median(v), "accepted_as_the_harness": same}
     if ref is not None:
         line["parity_vs_oracle"] = "bit-exact" if ok else "MISMATCH"
     print(json.dumps(line), flush=True)

@@ -65,6 +65,11 @@ class ClosedLoop:
         """Append items that load a fresh request into every slot: (slots, token lists, reset flags)."""
         return list(range(self.n_slots)), [self._new_request(s) for s in range(self.n_slots)], [1] * self.n_slots
 
+    def last_token(self, slot: int) -> int:
+        """The last token of the slot's text so far."""
+        cur = self.cursor[slot]
+        return int(self.truth[slot][cur - 1] if cur else self.prompt[slot][-1])
+
     def advance(self, out: Dict[str, np.ndarray]):
         """Consume one step's drafts (row i belongs to slot i).  Returns the append items of
         this step: accepted + bonus tokens per slot, then for every request that finished a
