@@ -181,21 +181,22 @@ class _PlainCall:
 
 
     def rotate(self, q, k, v, k_cache, v_cache, table, offsets, cached, freq, mask, positions, q_weight, k_weight, eps, interleaved,
-               scale, out, status) -> int:
+               scale, out, status):
         cache, dt = _cache_of(k_cache, v_cache, (4,)), k_cache.dtype
-        rows, n = _length(q, "q"), _length(offsets, "offsets") - 1
+        rows = _length(q, "q")
         b = _rows_of(rows, table, offsets, cached, mask, status)
         heads, D = _q_heads(q), k_cache.shape[-1]
         if heads > 65536 or freq.numel() > 64:
             raise TypeError("rotate: at most 65,536 heads and 64 frequencies")
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
         strides = [_heads(t, dt, (rows, h, D), name) for t, h, name in ((q, heads, "q"), (k, cache.kv_heads, "k"), (v, cache.kv_heads, "v"), (out, heads, "out"))]
         p = _RotateParams(heads, 2 * freq.numel(), int(interleaved), scale, eps, *strides)
         return self._lib.sd_rotate(
             C.byref(cache), C.byref(b), C.byref(p), q.data_ptr(), k.data_ptr(), v.data_ptr(), _array(freq, torch.float64, (freq.numel(),), "freq"),
             _array(positions, torch.int32, (rows,), "positions"), _array(q_weight, dt, (D,), "q_weight"),
-            _array(k_weight, dt, (D,), "k_weight"), out.data_ptr(), _stream())
+            _array(k_weight, dt, (D,), "k_weight"), out.data_ptr(), _stream()) or out
 
-    def attend(self, q, k_cache, v_cache, table, offsets, cached, mask, scale, window, sinks, shared, out, lse, status) -> int:
+    def attend(self, q, k_cache, v_cache, table, offsets, cached, mask, scale, window, sinks, shared, out, lse, status):
         cache, dt = _cache_of(k_cache, v_cache, (4,)), k_cache.dtype
         rows = _length(q, "q")
         b = _rows_of(rows, table, offsets, cached, mask, status)
@@ -203,36 +204,44 @@ class _PlainCall:
         for name, x in (("q_heads", heads), ("window", window), ("sinks", sinks), ("shared", shared)):
             if not 0 <= x <= (65536 if name == "q_heads" else 0x7FFFFFFF):
                 raise SuffixSpecError(-1, f"sd_attend: {name} {x}")
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        scale = max(D, 1) ** -0.5 if scale is None else scale
         p = _AttendParams(heads, scale, window, sinks, shared, _heads(q, dt, (rows, heads, D), "q"), _heads(out, dt, (rows, heads, D), "out"))
         lse = _array(lse, torch.float32, (rows, heads), "lse")
         size = self._lib.sd_attend_workspace(C.byref(cache), C.byref(b), C.byref(p))
         if size < 0:
             return size
         work = torch.empty(size, dtype=torch.uint8, device=q.device)
-        return self._lib.sd_attend(C.byref(cache), C.byref(b), C.byref(p), q.data_ptr(), out.data_ptr(), lse, work.data_ptr(), size, _stream())
+        return self._lib.sd_attend(C.byref(cache), C.byref(b), C.byref(p), q.data_ptr(), out.data_ptr(), lse, work.data_ptr(), size, _stream()) or out
 
-    def accept(self, logits, offsets, tokens, parents, targets, path, new_offsets, new_tokens, status) -> int:
+    def accept(self, logits, offsets, tokens, parents, out, status):
         if logits.dim() != 2 or tokens.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
             raise TypeError("accept: expected logits [rows, vocab] with adjacent entries and tokens [n, max_draft]")
         (rows, vocab), (n, M) = logits.shape, tokens.shape
         if logits.dtype not in _DTYPES or M > MAX_DRAFT or max(rows, vocab, n) > 0x7FFFFFFE:
             raise TypeError(f"accept: logits of {logits.dtype}, drafts of {M}")
         _here(logits, "logits")
+        if out is None:
+            i32 = dict(dtype=torch.int32, device=logits.device)
+            out = {"targets": torch.empty(rows, **i32), "path": torch.empty(n, M + 1, **i32),
+                   "offsets": torch.empty(n + 1, dtype=torch.int64, device=logits.device), "tokens": torch.empty(rows, **i32)}
+        targets, path, new_offsets, new_tokens = (out[k] for k in ("targets", "path", "offsets", "tokens"))
         args = [_array(t, dt, shape, name) for t, dt, shape, name in (
             (offsets, torch.int64, (n + 1,), "offsets"), (tokens, torch.int32, (n, M), "tokens"), (parents, torch.int32, (n, M), "parents"),
             (targets, torch.int32, (rows,), "targets"), (path, torch.int32, (n, M + 1), "path"), (new_offsets, torch.int64, (n + 1,), "new_offsets"),
             (new_tokens, torch.int32, (rows,), "new_tokens"), (status, torch.int32, (n,), "status"))]
-        return self._lib.sd_accept(n, rows, M, vocab, _DTYPES[logits.dtype], logits.stride(0) if rows > 1 else vocab, logits.data_ptr(), *args, _stream())
+        return self._lib.sd_accept(n, rows, M, vocab, _DTYPES[logits.dtype], logits.stride(0) if rows > 1 else vocab, logits.data_ptr(), *args, _stream()) or out
 
-    def commit(self, k_cache, v_cache, table, cached, path, new_cached, status) -> int:
+    def commit(self, k_cache, v_cache, table, cached, path, out, status):
         cache = _cache_of(k_cache, v_cache, (4, 5))
         if path.dim() != 2 or not 1 <= path.shape[1] <= MAX_DRAFT + 1 or table.dim() != 2:
             raise TypeError("commit: expected a path [n, max_draft + 1] and a table [n, pages]")
         n, M1 = path.shape
         b = _Rows(n, 0, M1 - 1, table.shape[1], None, _array(cached, torch.int32, (n,), "cached"),
                   _array(table, torch.int32, (n, table.shape[1]), "table"), None, _array(status, torch.int32, (n,), "status"))
+        out = torch.empty(cached.shape, dtype=cached.dtype, device=cached.device) if out is None else out
         return self._lib.sd_commit(C.byref(cache), C.byref(b), _array(path, torch.int32, (n, M1), "path"),
-                                   _array(new_cached, torch.int32, (n,), "new_cached"), _stream())
+                                   _array(out, torch.int32, (n,), "out"), _stream()) or out
 
 
 def _here(t: torch.Tensor, name: str) -> None:
@@ -373,13 +382,13 @@ def sd_speculate_noalloc(store: int, slots: torch.Tensor, P: int, alpha: float, 
         raise SuffixSpecError(rc, "sd_speculate_noalloc")
 
 
-def _made(name: str, args: tuple) -> None:
-    """The native call, or, where one of its tensors is not usual, the same call in Python; raises what its status says."""
-    rc = getattr(_call or _loaded(), name)(*args)
-    if rc is None:
-        rc = getattr(_PlainCall(library()), name)(*args)
-    if rc != 0:
-        raise SuffixSpecError(rc, "sd_" + name)
+def _made(name: str, result, args: tuple):
+    """What the native call gave; where one of its tensors was not usual (None), what the same call in Python gives.  Raises what a status says."""
+    if result is None:
+        result = getattr(_PlainCall(library()), name)(*args)
+    if type(result) is int:
+        raise SuffixSpecError(result, "sd_" + name)
+    return result
 
 
 def sd_rotate(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
@@ -390,10 +399,9 @@ def sd_rotate(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.
     """Queries q [rows, q_heads, head_dim], normed (where they have a weight) and turned to the rows' positions; keys likewise and values go to the
     rows' places in the cache [pages, page_size, kv_heads, head_dim].  freq: float64, radians per position of each pair (see
     rotary_frequencies); the first 2 * len(freq) elements of a head are turned.  offsets, cached, table, mask: the batch (see suffixspec.h).  out may be q."""
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _made("rotate", (q, k, v, k_cache, v_cache, table, offsets, cached, freq, mask, positions, q_weight, k_weight, eps, interleaved, scale, out, status))
-    return out
+    args = (q, k, v, k_cache, v_cache, table, offsets, cached, freq, mask, positions, q_weight, k_weight, eps, interleaved, scale, out, status)
+    got = (_call or _loaded()).rotate(*args)
+    return got if type(got) is torch.Tensor else _made("rotate", got, args)
 
 
 def sd_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, offsets: torch.Tensor, cached: torch.Tensor,
@@ -402,34 +410,27 @@ def sd_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, tab
     """Attention of the rows q [rows, q_heads, head_dim] of draft trees over their requests' caches under the mask of sd_speculate (None: each row
     sees those before it).  scale: 1 / sqrt(head_dim) unless given.  window, sinks: a row sees the last `window` positions and the first `sinks` (0: all).
     shared: so many first places of all requests are in the same pages and are read once for the batch."""
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if scale is None:
-        scale = q.shape[-1] ** -0.5
-    _made("attend", (q, k_cache, v_cache, table, offsets, cached, mask, scale, window, sinks, shared, out, lse, status))
-    return out
+    args = (q, k_cache, v_cache, table, offsets, cached, mask, scale, window, sinks, shared, out, lse, status)
+    got = (_call or _loaded()).attend(*args)
+    return got if type(got) is torch.Tensor else _made("attend", got, args)
 
 
 def sd_accept(logits: torch.Tensor, offsets: torch.Tensor, tokens: torch.Tensor, parents: torch.Tensor, *,
               out: Optional[Dict[str, torch.Tensor]] = None, status: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
     """Greedy verification of the drafts (tokens, parents: of sd_speculate) against logits [rows, vocab].  Returns targets [rows], path [n, max_draft + 1],
     and offsets [n + 1] and tokens [rows], which sd_step takes as they are."""
-    if out is None:
-        (n, M), rows, i32 = tokens.shape, logits.shape[0], dict(dtype=torch.int32, device=logits.device)
-        out = {"targets": torch.empty(rows, **i32), "path": torch.empty(n, M + 1, **i32),
-               "offsets": torch.empty(n + 1, dtype=torch.int64, device=logits.device), "tokens": torch.empty(rows, **i32)}
-    _made("accept", (logits, offsets, tokens, parents, out["targets"], out["path"], out["offsets"], out["tokens"], status))
-    return out
+    args = (logits, offsets, tokens, parents, out, status)
+    got = (_call or _loaded()).accept(*args)
+    return got if type(got) is dict else _made("accept", got, args)
 
 
 def sd_commit(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, cached: torch.Tensor, path: torch.Tensor, *,
               out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Keys and values of the accepted rows (path: of sd_accept) to where their sequences continue, in a cache
     [pages, page_size, kv_heads, head_dim] or, for all layers at once, [layers, pages, ...].  Returns the requests' lengths from now on; out may be cached."""
-    if out is None:
-        out = torch.empty(cached.shape, dtype=cached.dtype, device=cached.device)
-    _made("commit", (k_cache, v_cache, table, cached, path, out, status))
-    return out
+    args = (k_cache, v_cache, table, cached, path, out, status)
+    got = (_call or _loaded()).commit(*args)
+    return got if type(got) is torch.Tensor else _made("commit", got, args)
 
 
 def rotary_frequencies(rot_dim: int, base: float = 10000.0, *, device=None, factor: float = 1.0, original: int = 0, fast: float = 32.0,

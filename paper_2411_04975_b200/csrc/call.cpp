@@ -16,6 +16,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ops/empty.h>
 
+#include <algorithm>
+#include <cmath>
 #include <initializer_list>
 
 #include "suffixspec.h"
@@ -224,8 +226,9 @@ PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t na) {
 }
 
 // ---- the verifier's calls ---------------------------------------------------------------------
-// Each returns the entry point's status, or None where a tensor is not what is usual (its type, shape, strides or device): the same call
-// in Python then takes it, or says what is wrong with it.
+// Each returns the call's result (the output it was given, or one of its own making), or the entry point's status where that is an error, or None where a tensor is
+// not what is usual (its type, shape, strides or device): the same call in Python then takes it, or says what is wrong with it.  (Outputs made here: a call of one small
+// request is 2 us shorter than with them made in Python.)
 decltype(&sd_rotate) f_rotate;
 decltype(&sd_attend) f_attend;
 decltype(&sd_attend_workspace) f_attend_workspace;
@@ -257,6 +260,20 @@ T* array(PyObject* o, int device, c10::ScalarType type, std::initializer_list<in
         if (t.size(d++) != s) throw Unusual();
     return (T*)t.data_ptr();
 }
+
+// The output `o`, or a new one like `like` where it is None; a new reference in `result`.
+PyObject* made(PyObject* o, const at::Tensor& like) {
+    if (o != Py_None) { Py_INCREF(o); return o; }
+    return THPVariable_Wrap(at::empty(like.sizes(), like.options()));
+}
+PyObject* made(at::IntArrayRef shape, c10::ScalarType type, const at::Tensor& like) { return THPVariable_Wrap(at::empty(shape, like.options().dtype(type))); }
+
+// Given back where it is not handed out.
+struct Held {
+    PyObject* o;
+    ~Held() { Py_XDECREF(o); }
+    PyObject* release() { PyObject* r = o; o = nullptr; return r; }
+};
 
 // Rows of heads: [rows][heads][head_dim] with adjacent elements.
 void* heads_of(PyObject* o, int device, c10::ScalarType type, int64_t rows, int64_t heads, int64_t dim, int64_t* stride) {
@@ -315,7 +332,10 @@ sd_rows rows_of(int64_t rows, PyObject* table, PyObject* offsets, PyObject* cach
         const int device = current.device_index();               \
         void* st = current.stream();                             \
         int rc;                                                  \
+        PyObject* result = nullptr;                              \
         __VA_ARGS__                                              \
+        if (rc == 0) return result;                              \
+        Py_XDECREF(result);                                      \
         return PyLong_FromLong(rc);                              \
     } catch (const Unusual&) {                                   \
         Py_RETURN_NONE;                                          \
@@ -339,13 +359,15 @@ PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t na) {
         const void* dq = heads_of(a[0], device, type, R, q.size(1), D, p.q_stride);
         const void* dk = heads_of(a[1], device, type, R, c.kv_heads, D, p.k_stride);
         const void* dv = heads_of(a[2], device, type, R, c.kv_heads, D, p.v_stride);
-        void* out = heads_of(a[16], device, type, R, q.size(1), D, p.out_stride);
+        Held h = {made(a[16], q)};
+        void* out = heads_of(h.o, device, type, R, q.size(1), D, p.out_stride);
         const sd_rows b = rows_of(R, a[5], a[6], a[7], a[9], a[17], device);
         const auto* f = array<const double>(a[8], device, c10::kDouble, {freq.size(0)});
         const auto* pos = array<const int32_t>(a[10], device, c10::kInt, {R});
         const void* qw = array<const void>(a[11], device, type, {D});
         const void* kw = array<const void>(a[12], device, type, {D});
         rc = f_rotate(&c, &b, &p, dq, dk, dv, f, pos, qw, kw, out, st);
+        if (rc == 0) result = h.release();
     })
 }
 
@@ -359,13 +381,15 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t na) {
         const int64_t R = q.size(0);
         sd_attend_params p = {};
         if (q.size(1) > 65536) throw Unusual();
-        p.q_heads = (int32_t)q.size(1); p.scale = (float)real(a[7]);
+        p.q_heads = (int32_t)q.size(1);
+        p.scale = a[7] == Py_None ? 1.0f / std::sqrt((float)std::max(c.head_dim, 1)) : (float)real(a[7]);
         const long long way[3] = {integer(a[8]), integer(a[9]), integer(a[10])};
         for (const long long w : way)
             if (w < 0 || w > 0x7FFFFFFF) throw Unusual();
         p.window = (int32_t)way[0]; p.sinks = (int32_t)way[1]; p.shared = (int32_t)way[2];
         const void* dq = heads_of(a[0], device, type, R, q.size(1), c.head_dim, p.q_stride);
-        void* out = heads_of(a[11], device, type, R, q.size(1), c.head_dim, p.out_stride);
+        Held h = {made(a[11], q)};
+        void* out = heads_of(h.o, device, type, R, q.size(1), c.head_dim, p.out_stride);
         const sd_rows b = rows_of(R, a[3], a[4], a[5], a[6], a[13], device);
         auto* lse = array<float>(a[12], device, c10::kFloat, {R, q.size(1)});
         const int64_t bytes = f_attend_workspace(&c, &b, &p);
@@ -374,12 +398,13 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t na) {
             const at::Tensor w = at::empty({bytes}, q.options().dtype(c10::kByte));
             rc = f_attend(&c, &b, &p, dq, out, lse, w.data_ptr(), bytes, st);
         }
+        if (rc == 0) result = h.release();
     })
 }
 
-// accept(logits, offsets, tokens, parents, targets, path, new_offsets, new_tokens, status)
+// accept(logits, offsets, tokens, parents, out, status)
 PyObject* accept(PyObject*, PyObject* const* a, Py_ssize_t na) {
-    if (!count_is(na, 9, "accept")) return nullptr;
+    if (!count_is(na, 6, "accept")) return nullptr;
     VERIFIER_CALL({
         const at::Tensor &x = cuda_tensor(a[0], device, 2), &tok = cuda_tensor(a[2], device, 2);
         const int64_t R = x.size(0), n = tok.size(0), M = tok.size(1);
@@ -387,13 +412,24 @@ PyObject* accept(PyObject*, PyObject* const* a, Py_ssize_t na) {
         const auto* off = array<const int64_t>(a[1], device, c10::kLong, {n + 1});
         const auto* tokens = array<const int32_t>(a[2], device, c10::kInt, {n, M});
         const auto* parents = array<const int32_t>(a[3], device, c10::kInt, {n, M});
-        auto* targets = array<int32_t>(a[4], device, c10::kInt, {R});
-        auto* path = array<int32_t>(a[5], device, c10::kInt, {n, M + 1});
-        auto* new_offsets = array<int64_t>(a[6], device, c10::kLong, {n + 1});
-        auto* new_tokens = array<int32_t>(a[7], device, c10::kInt, {R});
-        auto* status = array<int32_t>(a[8], device, c10::kInt, {n});
+        static PyObject* const keys[4] = {PyUnicode_InternFromString("targets"), PyUnicode_InternFromString("path"), PyUnicode_InternFromString("offsets"),
+                                          PyUnicode_InternFromString("tokens")};
+        Held h = {a[4] == Py_None ? PyDict_New() : (Py_INCREF(a[4]), a[4])};
+        Held o[4] = {};
+        for (int k = 0; k < 4; ++k) {
+            if (a[4] == Py_None) {
+                o[k].o = k == 0 || k == 3 ? made({R}, c10::kInt, x) : k == 1 ? made({n, M + 1}, c10::kInt, x) : made({n + 1}, c10::kLong, x);
+                if (!h.o || !o[k].o || PyDict_SetItem(h.o, keys[k], o[k].o)) throw Raised();
+            } else if (!(o[k].o = PyObject_GetItem(h.o, keys[k]))) throw Raised();
+        }
+        auto* targets = array<int32_t>(o[0].o, device, c10::kInt, {R});
+        auto* path = array<int32_t>(o[1].o, device, c10::kInt, {n, M + 1});
+        auto* new_offsets = array<int64_t>(o[2].o, device, c10::kLong, {n + 1});
+        auto* new_tokens = array<int32_t>(o[3].o, device, c10::kInt, {R});
+        auto* status = array<int32_t>(a[5], device, c10::kInt, {n});
         rc = f_accept((int32_t)n, (int32_t)R, (int32_t)M, (int32_t)x.size(1), type_of(x.scalar_type()), R > 1 ? x.stride(0) : x.size(1), x.data_ptr(), off,
                       tokens, parents, targets, path, new_offsets, new_tokens, status, st);
+        if (rc == 0) result = h.release();
     })
 }
 
@@ -410,9 +446,11 @@ PyObject* commit(PyObject*, PyObject* const* a, Py_ssize_t na) {
         b.d_table = array<const int32_t>(a[2], device, c10::kInt, {n, tab.size(1)});
         b.d_cached = array<const int32_t>(a[3], device, c10::kInt, {n});
         const auto* d_path = array<const int32_t>(a[4], device, c10::kInt, {n, M1});
-        auto* out = array<int32_t>(a[5], device, c10::kInt, {n});
+        Held h = {made(a[5], cuda_tensor(a[3], device, 1))};
+        auto* out = array<int32_t>(h.o, device, c10::kInt, {n});
         b.d_status = array<int32_t>(a[6], device, c10::kInt, {n});
         rc = f_commit(&c, &b, d_path, out, st);
+        if (rc == 0) result = h.release();
     })
 }
 
