@@ -90,12 +90,17 @@ struct Shape {
     static constexpr int HALVES = D / 64;
     static constexpr int SLOT_BYTES = TILE * D * 2, HALF_BYTES = TILE * 128;
     static constexpr int SLOTS = D == 128 ? 5 : 8;
+    // Barriers of the ring: for two rounds of it.  A wait tells a barrier's phase from the one before it and from no other.  With a barrier a slot, a group that leaves tiles
+    // to the other one could take a slot that still waits for its last but one filling as filled (copies do not land in order), and the warp that copies values, slots that
+    // have turns with the keys, one whose last but one reader is late as free.  What lies two rounds back, though, is always behind: keys are copied in order, those of a
+    // tile when the readers of the ring's round before are through, and no group gets ahead of the other by more than that.
+    static constexpr int BARS = 2 * SLOTS;
     static constexpr int Q_BYTES = 128 * D * 2;
     static constexpr int RING = 0, Q = SLOTS * SLOT_BYTES, REST = Q + 2 * Q_BYTES;
 };
 
 struct Rest {                     // of shared memory
-    uint64_t full[8], empty[8], s_full[2], p_ready[2], o_done[2], q_full[2], q_empty[2], unit_full[UNITS], unit_empty[UNITS], meet, group_meet[2], over[2], lead;
+    uint64_t full[16], empty[16], s_full[2], p_ready[2], o_done[2], q_full[2], q_empty[2], unit_full[UNITS], unit_empty[UNITS], meet, group_meet[2], over[2], lead;
     uint32_t tmem;
     int stop;
     int begun[2];                 // the group has begun its results itself: the first product adds to them
@@ -189,11 +194,11 @@ struct Lines {
     }
     // Tile k of the unit, whose pages have been looked up, and a look at the next.  False: given up.
     __device__ __forceinline__ bool copy(const Unit& u, int k, bool wide) {
-        const uint32_t e = it % S::SLOTS, bar = bw_smem(&s->full[e]);
+        const uint32_t e = it % S::SLOTS, bar = bw_smem(&s->full[it % S::BARS]), before = it - S::SLOTS;
         const int boxes = __popc(__ballot_sync(~0u, here));
-        if (it >= S::SLOTS && !bw_wait_warp(bw_smem(&s->empty[e]), (it / S::SLOTS - 1) & 1, &s->stop)) return false;
+        if (it >= S::SLOTS && !bw_wait_warp(bw_smem(&s->empty[before % S::BARS]), (before / S::BARS) & 1, &s->stop)) return false;
         if ((threadIdx.x & 31) == 0) {
-            if (!wide) bw_arrive(bw_smem(&s->empty[e]));          // (for the group that does not use it)
+            if (!wide) bw_arrive(bw_smem(&s->empty[it % S::BARS]));          // (for the group that does not use it)
             bw_arrive_expect(bar, boxes * a.box * 128);
         }
         if ((unsigned)page >= (unsigned)a.c.n_pages) page = a.c.n_pages;                  // (a page that is none: beyond the last, where a copy fills in zeros)
@@ -207,9 +212,9 @@ struct Lines {
     }
     // Given up: this warp's copies in flight come to their end.
     __device__ __noinline__ void drain() {
-        for (uint32_t k = it >= 2 * S::SLOTS ? it - 2 * S::SLOTS : v; k < it; k += 2) {
+        for (uint32_t k = it >= S::BARS ? it - S::BARS : v; k < it; k += 2) {
             int never = 0;
-            bw_wait_slow(bw_smem(&s->full[k % S::SLOTS]), (k / S::SLOTS) & 1, &never, 200000000ll);
+            bw_wait_slow(bw_smem(&s->full[k % S::BARS]), (k / S::BARS) & 1, &never, 200000000ll);
         }
     }
 };
@@ -461,7 +466,7 @@ __device__ bool multiply(const AttendArgs& a, Rest* s, uint32_t ring, uint32_t q
             const int next = j + step;
             const uint32_t v = it + 2 * j + 1, k = it + 2 * next;
             if (j >= 0) {
-                if (!bw_wait_warp(bw_smem(&s->full[v % S::SLOTS]), (v / S::SLOTS) & 1, &s->stop)) return false;
+                if (!bw_wait_warp(bw_smem(&s->full[v % S::BARS]), (v / S::BARS) & 1, &s->stop)) return false;
                 if (!bw_wait_warp(bw_smem(&s->p_ready[w]), count++ & 1, &s->stop)) return false;
                 bw_fence_after();
                 const bool add = j >= step || uniform(*(volatile int*)&s->begun[w]);
@@ -470,7 +475,7 @@ __device__ bool multiply(const AttendArgs& a, Rest* s, uint32_t ring, uint32_t q
                 for (int i = 0; i < TILE / 16; ++i) bw_mma_ts(O0, S0 + i * 8, vd + (i * 2048 >> 4), pv, add || i > 0, leader);
             }
             if (next < tiles) {
-                if (!bw_wait_warp(bw_smem(&s->full[k % S::SLOTS]), (k / S::SLOTS) & 1, &s->stop)) return false;
+                if (!bw_wait_warp(bw_smem(&s->full[k % S::BARS]), (k / S::BARS) & 1, &s->stop)) return false;
                 bw_fence_after();
                 const uint64_t qd = bw_desc(q + mine * S::Q_BYTES), kd = bw_desc(ring + k % S::SLOTS * S::SLOT_BYTES);
 #pragma unroll
@@ -479,11 +484,11 @@ __device__ bool multiply(const AttendArgs& a, Rest* s, uint32_t ring, uint32_t q
                     bw_mma(S0, qd + off, kd + off, qk, i > 0, leader);
                 }
                 bw_commit(bw_smem(&s->s_full[w]), leader);
-                bw_commit(bw_smem(&s->empty[k % S::SLOTS]), leader);
+                bw_commit(bw_smem(&s->empty[k % S::BARS]), leader);
                 if (next + step >= tiles) bw_commit(bw_smem(&s->q_empty[mine]), leader);
             }
             if (j >= 0) {
-                bw_commit(bw_smem(&s->empty[v % S::SLOTS]), leader);
+                bw_commit(bw_smem(&s->empty[v % S::BARS]), leader);
                 if (next >= tiles) bw_commit(bw_smem(&s->o_done[w]), leader);
             }
         }
@@ -549,6 +554,7 @@ struct Softmax {
 // The warp's results times alpha.  (Seldom: out of line.)
 template <int D>
 __device__ __noinline__ void scale_results(uint32_t O0, float alpha) {
+    __syncwarp();
 #pragma unroll 1
     for (int c = 0; c < D; c += 16) {
         uint32_t y[16];
@@ -572,11 +578,13 @@ __device__ __forceinline__ void most_of(const uint32_t* v, float* m) {
 // A tile that not every row sees whole: scores that a row does not see become -inf, in tensor memory, so that the rest is the same for all tiles.  Returns the largest.
 // (Out of line, as all that follows for such tiles: in the loop over tiles its instructions and registers cost whole tiles a quarter of their time.)
 __device__ __noinline__ float hide(const Sight& see, int place, uint32_t S0) {
+    __syncwarp();
     float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     uint32_t x[32], y[32];
     auto hidden = [&](uint32_t* v, int c) {
         const uint32_t word = see.word(place + c);
         const bool whole = __all_sync(~0u, word == ~0u);
+        __syncwarp();
         bw_wait_ld32(v);
         if (c + 32 < TILE) bw_ld32(S0 + c + 32, v == x ? y : x);
         if (!whole) {
@@ -607,6 +615,7 @@ struct Border {
 // Their part in the results, which begin here if it is the first tile.
 template <class T, int D>
 __device__ __noinline__ void add_lines(const uint32_t* lines, const Sight& see, const Border& b) {
+    __syncwarp();
     if (b.first)
 #pragma unroll 1
         for (int c = 0; c < D; c += 8) {
@@ -621,6 +630,7 @@ __device__ __noinline__ void add_lines(const uint32_t* lines, const Sight& see, 
         if (!(lines[l / 32] >> l % 32 & 1)) continue;
         const bool seen = see.word(b.place + l) & 1;
         if (!__any_sync(~0u, seen)) continue;
+        __syncwarp();
         const uint32_t two = bw_ld1(b.S0 + l / 2);
         const float2 weight = Elem<T>::up(two);
         const float p = l % 2 ? weight.y : weight.x;
@@ -731,6 +741,7 @@ __device__ bool Softmax<T, D>::run(int n) {
             }
             if (wide && j == 0 && !masked) bw_arrive_warp(bw_smem(&s->lead));
             const float power = (top == -INFINITY ? 0.f : top * scale) - BIAS;
+            __syncwarp();
             const float2 by = make_float2(scale, scale), less = make_float2(-power, -power);
             float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
             auto weigh = [&](uint32_t* v) {
@@ -755,10 +766,11 @@ __device__ bool Softmax<T, D>::run(int n) {
             }
             sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
         }
+        __syncwarp();
         if (masked) {
             bw_wait_st();
             const uint32_t vs = it + 2 * (wide ? j >> 1 : j) + 1;
-            Border b = {base + S::RING + vs % S::SLOTS * S::SLOT_BYTES, S0, O0, bw_smem(&s->full[vs % S::SLOTS]), (vs / S::SLOTS) & 1, meets, group_meets, w, t, number * TILE, busy, j < 2, wide};
+            Border b = {base + S::RING + vs % S::SLOTS * S::SLOT_BYTES, S0, O0, bw_smem(&s->full[vs % S::BARS]), (vs / S::BARS) & 1, meets, group_meets, w, t, number * TILE, busy, j < 2, wide};
             if (!clear_lines<T, D>(s, see, b)) return false;
             meets = b.meets; group_meets = b.group_meets;
         }
@@ -808,6 +820,7 @@ __device__ __forceinline__ bool Softmax<T, D>::finish(const Unit& u, float top, 
     T* out = (T*)a.out + (u.begin + r) * a.p.out_stride[0] + h * a.p.out_stride[1];
     float* part = to == SLOT ? a.part + ((long long)u.slot * 256 + mrow) * D : a.plane[u.slot & 1] + at * D;
     uint32_t x[16], z[16];
+    __syncwarp();
     bw_ld16(A + c0, x);
     if (two) bw_ld16(A + TILE + c0, z);
 #pragma unroll 1
@@ -854,7 +867,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
     Rest* s = (Rest*)(smem + S::REST);
     const int t = threadIdx.x, warp = uniform(t >> 5), lane = t & 31;
     if (t == 0) {
-        for (int e = 0; e < S::SLOTS; ++e) { bw_bar_init(bw_smem(&s->full[e]), 1); bw_bar_init(bw_smem(&s->empty[e]), 2); }
+        for (int e = 0; e < S::BARS; ++e) { bw_bar_init(bw_smem(&s->full[e]), 1); bw_bar_init(bw_smem(&s->empty[e]), 2); }
         for (int e = 0; e < 2; ++e) {
             bw_bar_init(bw_smem(&s->s_full[e]), 1); bw_bar_init(bw_smem(&s->p_ready[e]), 4); bw_bar_init(bw_smem(&s->o_done[e]), 1);
             bw_bar_init(bw_smem(&s->q_full[e]), 1); bw_bar_init(bw_smem(&s->q_empty[e]), 2); bw_bar_init(bw_smem(&s->group_meet[e]), 4);

@@ -16,6 +16,7 @@ __device__ __forceinline__ void bw_arrive(uint32_t bar) { asm volatile("mbarrier
 __device__ __forceinline__ void bw_arrive_warp(uint32_t bar) {
     __syncwarp();
     if ((threadIdx.x & 31) == 0) bw_arrive(bar);
+    __syncwarp();                                                 // (together again: what follows may be for whole warps only)
 }
 __device__ __forceinline__ void bw_arrive_expect(uint32_t bar, uint32_t bytes) { asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory"); }
 

@@ -267,6 +267,22 @@ def test_attend_repeats_bit_for_bit():
         assert torch.equal(first, sfx.sd_attend(*a, mask=b.mask_arg()))
 
 
+@pytest.mark.parametrize("head,kv_heads,group", [(128, 8, 4), (64, 8, 2), (128, 2, 32)])
+def test_attend_long_lists_under_load(head, kv_heads, group):
+    """Units of one and of two tiles of rows, with few and with many tiles, in turns, when every multiprocessor fetches: copies land in any order, and groups overtake one another."""
+    for seed in range(3):
+        rng = np.random.default_rng(900 + seed)
+        n = 64
+        b = R.Batch(rng.integers(100, 4000, n).tolist(), rng.integers(0, 65, n).tolist(), head=head, kv_heads=kv_heads, group=group, page=64, seed=900 + seed)
+        k, v = b.caches()
+        a = (b.q.cuda(), k, v, *b.args())
+        status = torch.empty(n, dtype=torch.int32, device="cuda:0")
+        first = check_attend(b, caches=(k, v))[0] if seed == 0 else sfx.sd_attend(*a, mask=b.mask_arg())
+        for _ in range(200):
+            again = sfx.sd_attend(*a, mask=b.mask_arg(), status=status)
+            assert torch.equal(first, again) and not status.any()
+
+
 def test_attend_fuzz():
     rng = np.random.default_rng(22)
     for s in range(60):
