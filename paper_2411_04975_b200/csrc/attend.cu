@@ -926,8 +926,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
 }
 
 // ---- joining -------------------------------------------------------------------------------
-// A warp per packed row of a cut unit: its parts by their sums.
-constexpr int JOIN_ROWS = 8, MOST_BLOCKS = 1024;
+// A warp per packed row of a cut unit: its parts by their sums.  Rows of few calls are many, so that what a row takes is the latency of its loads: the cut, then its
+// sums and eight parts at once (one token over a long context 23.5 -> 19.5 us against a kernel that first looked up where a row belongs and loaded parts behind the sums).
+constexpr int JOIN_ROWS = 8, JOIN_BLOCKS = 16, AHEAD = 8, MOST_BLOCKS = 1024;
 
 template <class T, int D>
 __device__ void join_row(const AttendArgs& a, const Cut& c, int m, int lane, bool planes) {
@@ -937,9 +938,21 @@ __device__ void join_row(const AttendArgs& a, const Cut& c, int m, int lane, boo
     auto slot = [&](int k) { return (long long)(2 * (c.first + k) + (k == 0)) * 256 + mrow; };
     const int parts = c.last - c.first + 1;
     float top = -INFINITY, sum = 0.f, x[E] = {};                  // running, 32 parts at a time
+#pragma unroll 1
     for (int first = 0; first < parts; first += 32) {
         const int n = min(32, parts - first);
         const float v = lane < n ? a.part_lse[slot(first + lane)] : -INFINITY;
+        float z[AHEAD][E];
+        auto fetch = [&](int k0) {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (k0 + k < n) {
+                    const float* y = a.part + slot(first + k0 + k) * D + lane * E;
+#pragma unroll
+                    for (int e = 0; e < E; e += 2) { const float2 two = *(const float2*)(y + e); z[k][e] = two.x; z[k][e + 1] = two.y; }
+                }
+        };
+        fetch(0);                                                 // (on their way together with the sums)
         float most = v;
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
@@ -952,15 +965,18 @@ __device__ void join_row(const AttendArgs& a, const Cut& c, int m, int lane, boo
         top = most;
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] *= keep;
-#pragma unroll 4
-        for (int k = 0; k < n; ++k) {
-            const float* y = a.part + slot(first + k) * D + lane * E;
-            const float g = __shfl_sync(~0u, f, k);
-            float z[E];
+#pragma unroll 1
+        for (int k0 = 0;;) {
 #pragma unroll
-            for (int e = 0; e < E; e += 2) { const float2 two = *(const float2*)(y + e); z[e] = two.x; z[e + 1] = two.y; }
+            for (int k = 0; k < AHEAD; ++k) {
+                const float g = __shfl_sync(~0u, f, (k0 + k) & 31);
+                if (k0 + k < n && g != 0.f)                       // (0: a part in which the row sees nothing)
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] += g == 0.f ? 0.f : g * z[e];              // (a part in which the row sees nothing)
+                    for (int e = 0; e < E; ++e) x[e] += g * z[k][e];
+            }
+            k0 += AHEAD;
+            if (k0 >= n) break;
+            fetch(k0);
         }
     }
     const float inv = sum == 0.f ? 0.f : rcp(sum);
@@ -982,39 +998,14 @@ __device__ void join_row(const AttendArgs& a, const Cut& c, int m, int lane, boo
     }
 }
 
+// JOIN_BLOCKS blocks for each place that a cut may have: most find none.  (With 8 a long context whose rows are cut 18 times takes 3 us longer, with 32 small calls 1 us.)
 template <class T, int D>
 __global__ void __launch_bounds__(32 * JOIN_ROWS) join_cuts_kernel(const __grid_constant__ AttendArgs a, bool planes, int blocks) {
     sd_chain_begin();
-    __shared__ int s_end[MOST_BLOCKS], s_warp[JOIN_ROWS];         // packed rows of the cuts up to each
-    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    int base = 0;
-    for (int first = 0; first < blocks; first += 32 * JOIN_ROWS) {
-        int rows = 0;
-        if (first + t < blocks) {
-            const Cut c = a.cuts[first + t];
-            if (c.last >= c.first) rows = c.rows * a.group;
-        }
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int x = __shfl_up_sync(~0u, rows, d);
-            if (lane >= d) rows += x;
-        }
-        if (lane == 31) s_warp[warp] = rows;
-        __syncthreads();
-        for (int w = 0; w < warp; ++w) rows += s_warp[w];
-        if (first + t < blocks) s_end[first + t] = base + rows;
-        __syncthreads();
-        base = s_end[min(first + 32 * JOIN_ROWS, blocks) - 1];
-    }
-    for (int m = blockIdx.x * JOIN_ROWS + warp; m < base; m += gridDim.x * JOIN_ROWS) {
-        int lo = 0, hi = blocks - 1;                              // the first cut that ends behind m
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (s_end[mid] > m) hi = mid;
-            else lo = mid + 1;
-        }
-        join_row<T, D>(a, a.cuts[lo], m - (lo ? s_end[lo - 1] : 0), lane, planes);
-    }
+    const Cut c = a.cuts[blockIdx.x % blocks];
+    if (c.last < c.first) return;
+#pragma unroll 1
+    for (int m = blockIdx.x / blocks * JOIN_ROWS + (threadIdx.x >> 5); m < c.rows * a.group; m += gridDim.x / blocks * JOIN_ROWS) join_row<T, D>(a, c, m, threadIdx.x & 31, planes);
 }
 
 // With a shared prefix: it and what is behind it, a warp per row and head.
@@ -1140,9 +1131,8 @@ int launch(const AttendArgs& a, const Room& r, cudaStream_t st) {
     SD_CUDA_OK(cudaFuncSetAttribute(attend_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D>()));
     SD_CUDA_OK(sd_launch(attend_kernel<T, D>, r.blocks, THREADS, smem_bytes<D>(), st, a, mk, mv, mq));
     if (a.b.rows == 0) return SD_OK;
-    // (Blocks for the rows that there can be, or four a multiprocessor.)
-    const long long rows = std::min((long long)a.b.rows * a.p.q_heads, (long long)r.blocks * 2 * a.tile_rows * a.group);
-    SD_CUDA_OK(sd_launch(join_cuts_kernel<T, D>, (unsigned)std::min((rows + JOIN_ROWS - 1) / JOIN_ROWS, 4ll * r.blocks), 32 * JOIN_ROWS, 0, st, a, r.planes, r.blocks));
+    const long long rows = std::min((long long)a.b.rows, 2ll * a.tile_rows) * a.group;  // packed ones of a cut
+    SD_CUDA_OK(sd_launch(join_cuts_kernel<T, D>, r.blocks * (unsigned)std::min((rows + JOIN_ROWS - 1) / JOIN_ROWS, (long long)JOIN_BLOCKS), 32 * JOIN_ROWS, 0, st, a, r.planes, r.blocks));
     if (r.planes) SD_CUDA_OK(sd_launch(join_planes_kernel<T, D>, a.b.rows, 256, 0, st, a));
     return SD_OK;
 }
