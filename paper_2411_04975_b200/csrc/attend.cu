@@ -1071,8 +1071,9 @@ int room_for(const sd_cache* c, const sd_rows* b, const sd_attend_params* p, Roo
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return SD_ERR_CUDA;
     // all of the list, at the longest lengths that the tables hold
     const long long longest = ((long long)b->table_stride * c->page_size + TILE - 1) / TILE + 1, most = 2 * (128 / (p->q_heads / c->kv_heads));
-    const long long units = c->kv_heads * 2 * (b->n + (b->rows + most - 1) / most);
-    if (units > (1ll << 31) / (longest * WIDE + ENDS)) return SD_ERR_CAPACITY;
+    // (as many rows as each request can have: offsets that descend may give rows to more than one)
+    const long long units = c->kv_heads * ((long long)b->n * ((b->max_draft + most) / most) + (b->rows + most - 1) / most);
+    if (units > (1ll << 30) / (longest * WIDE + ENDS)) return SD_ERR_CAPACITY;
     r->planes = p->shared >= TILE && !p->window;
     r->blocks = (int)std::max(1ll, std::min((long long)std::min(sms, MOST_BLOCKS), (units * (longest * WIDE + ENDS) + LEAST - 1) / LEAST));
     int64_t at = 0;
@@ -1119,7 +1120,7 @@ bool map_of_queries(CUtensorMap* m, const AttendArgs& a) {
     const cuuint64_t dims[3] = {(cuuint64_t)a.c.head_dim, (cuuint64_t)a.p.q_heads, (cuuint64_t)std::max(a.b.rows, 1)};
     const cuuint64_t bytes[2] = {(cuuint64_t)(a.p.q_heads > 1 ? a.p.q_stride[1] : a.c.head_dim) * 2, (cuuint64_t)(a.b.rows > 1 ? a.p.q_stride[0] : (int64_t)a.p.q_heads * a.c.head_dim) * 2};
     const cuuint32_t shape[3] = {64, (cuuint32_t)a.group, (cuuint32_t)a.tile_rows}, step[3] = {1, 1, 1};
-    return f(m, a.c.dtype == SD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(a.q), dims, bytes, shape, step,
+    return f(m, a.c.dtype == SD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(a.b.rows ? a.q : a.c.d_k), dims, bytes, shape, step,
              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

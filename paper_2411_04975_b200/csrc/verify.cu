@@ -355,7 +355,7 @@ __global__ void __launch_bounds__(WALK_THREADS) walk_kernel(const WalkArgs a) {
         __syncthreads();
         x += s_base;
         for (int w = 0; w < warp; ++w) x += s_sum[w];
-        if (first + t < hi_i) a.new_offsets[first + t + 1] = x;
+        if (first + t < hi_i) a.new_offsets[first + t + 1] = min(x, (long long)a.rows);   // (more where offsets that descend give rows to two requests)
         __syncthreads();
         if (t == WALK_THREADS - 1) s_base = x;
         __syncthreads();

@@ -628,6 +628,49 @@ def test_arguments_that_are_refused():
         sfx.sd_commit(k, v, table, cached.long(), torch.zeros(2, 4, dtype=torch.int32, device="cuda:0"))
 
 
+def test_accept_rows_that_two_requests_claim():
+    """Offsets that descend: what they give to two requests is not written beyond the arrays."""
+    dev = lambda a, dt=torch.int32: torch.tensor(a, dtype=dt, device="cuda:0")    # noqa: E731
+    logits = torch.zeros(5, 8, device="cuda:0")
+    logits[torch.arange(5), torch.arange(1, 6)] = 1.0
+    tokens, parents = dev([[1, 2, 3, 4]] * 40), dev([[-1, 0, 1, 2]] * 40)
+    offsets = dev(([0, 5, 0, 0] * 10) + [5], torch.int64)
+    buf, status = dev([77] * 300), dev([99] * 40)
+    out = dict(targets=dev([0] * 5), path=dev([[0] * 5] * 40), offsets=dev([0] * 41, torch.int64), tokens=buf[:5])
+    sfx.sd_accept(logits, offsets, tokens, parents, out=out, status=status)
+    assert (buf[5:] == 77).all() and out["tokens"].tolist() == [1, 2, 3, 4, 5]
+    assert status.tolist() == [0, 16, 0, 0] * 10
+    ends = out["offsets"].tolist()
+    assert ends == sorted(ends) and ends[0] == 0 and ends[1:] == [5] * 40
+
+
+def test_attend_rows_that_two_requests_claim():
+    b = R.Batch([300, 0, 200, 0, 250], [9, -1, 9, -1, 9], head=64, seed=71)
+    k, v = b.caches()
+    table, _, cached = b.args()
+    offsets = torch.tensor([0, 10, 0, 0, 0, 10], dtype=torch.int64, device="cuda:0")
+    status = torch.full((5,), 99, dtype=torch.int32, device="cuda:0")
+    out = sfx.sd_attend(b.q.cuda(), k, v, table, offsets, cached, mask=b.mask_arg(), status=status)
+    assert status.tolist() == [0, 16, 0, 0, 0] and out.shape == b.q.shape
+
+
+def test_attend_without_rows_tells_the_status():
+    b = R.Batch([3, 40], [2, 4], seed=72)
+    k, v = b.caches()
+    table, _, cached = b.args()
+    status = torch.full((2,), 99, dtype=torch.int32, device="cuda:0")
+    sfx.sd_attend(b.q.cuda()[:0], k, v, table, torch.zeros(3, dtype=torch.int64, device="cuda:0"), cached, status=status)
+    assert status.tolist() == [0, 0]
+    status.fill_(99)
+    sfx.sd_attend(b.q.cuda()[:0], k, v, table, torch.tensor([0, 0, 2], device="cuda:0"), cached, status=status)
+    assert status.tolist() == [0, 16]
+
+
+@pytest.mark.parametrize("group,head", [(128, 64), (100, 128), (65, 64), (43, 128), (127, 64)])
+def test_attend_many_heads_of_one(group, head):
+    check_attend(R.Batch([200, 3, 129, 1000], [4, 0, 17, 64], kv_heads=1, group=group, head=head, seed=73))
+
+
 def test_calls_through_ctypes_alone(monkeypatch):
     """The conversions in Python, which stand in where the native module cannot be had."""
     from paper_2411_04975_b200 import binding

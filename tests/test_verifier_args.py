@@ -47,6 +47,13 @@ def test_attend_refuses(lib, bad):
     assert attend(lib, c, r, **(bad if bad in BAD_ATTEND else {})) == -1
 
 
+@pytest.mark.parametrize("bad", [dict(q_heads=130), dict(q_heads=258), dict(scale=float("inf")), dict(q_stride=(0, 64)), dict(q_stride=(256, 0)), dict(q_stride=(256, -64)),
+                                 dict(q_stride=(1 << 38, 64))], ids=str)
+def test_attend_refuses_heads_and_strides(lib, bad):
+    c = cache(kv_heads=1) if bad.get("q_heads") == 130 else cache()
+    assert attend(lib, c, rows(), **bad) == -1
+
+
 def test_attend_refuses_null_structs(lib):
     assert lib.sd_attend(None, None, None, None, None, None, None, 0, None) == -1
     assert lib.sd_attend_workspace(None, None, None) == -1
