@@ -294,7 +294,8 @@ int sd_speculate_noalloc(sd_store* store, int32_t n, const int32_t* d_slot, cons
  * no sense (offsets that descend or leave the row arrays, more rows than 1 + max_draft, a negative length, places
  * beyond its table) gets SD_STATUS_BAD_ROWS, and its rows stay as they were.  Of a page outside the cache nothing is
  * read or written, and the request gets SD_STATUS_BAD_PAGE; rows that should have seen it hold nothing of use.  Row arrays
- * may be longer than d_offsets[n]: rows behind it are not touched.
+ * may be longer than d_offsets[n]: rows behind it are not touched.  Where offsets that descend give rows to two requests, these rows hold
+ * nothing of use.  Memory is that of the current device.
  */
 enum { SD_BF16 = 1, SD_FP16 = 2, SD_FP32 = 3 };
 
@@ -333,12 +334,12 @@ typedef struct {
     int32_t interleaved;          /* pairs (2j, 2j + 1); else (j, j + rot_dim / 2)    */
     float scale;                  /* factor of the turned elements (long contexts)    */
     float eps;                    /* of the norms                                     */
-    int64_t q_stride[2], k_stride[2], v_stride[2], out_stride[2];   /* elements from row to row, head to head: multiples of 8 */
+    int64_t q_stride[2], k_stride[2], v_stride[2], out_stride[2];   /* elements from row to row, head to head: multiples of 8; of out > 0 where there is more than one */
 } sd_rotate_params;
 
 typedef struct {
-    int32_t q_heads;
-    float scale;                  /* factor of the scores, usually 1 / sqrt(head_dim) */
+    int32_t q_heads;              /* as above; at most 128 to a head of the cache     */
+    float scale;                  /* factor of the scores, usually 1 / sqrt(head_dim); finite */
     int32_t window;               /* a row at position x sees positions > x - window; */
                                   /* 0: all                                           */
     int32_t sinks;                /* ... and always the positions below this          */
@@ -346,7 +347,7 @@ typedef struct {
                                   /* the same pages (one prompt for all): their keys  */
                                   /* are read once for the batch.  0 .. every         */
                                   /* d_cached[i] of a request with rows               */
-    int64_t q_stride[2], out_stride[2];     /* elements from row to row, head to head: multiples of 8 */
+    int64_t q_stride[2], out_stride[2];     /* elements from row to row, head to head: multiples of 8, > 0 where there is more than one */
 } sd_attend_params;
 
 /*
@@ -376,7 +377,8 @@ int sd_rotate(const sd_cache* cache, const sd_rows* rows, const sd_rotate_params
  *   d_q, d_out   [rows][q_heads][head_dim], by their strides; d_out may be d_q with the same strides
  *   d_lse        float[rows][q_heads] or NULL: log of the sum of exp(score), -inf for a row that sees nothing
  *   d_workspace  sd_attend_workspace() bytes, 256-byte aligned, undefined before and after; a call needs one of its own as long as it runs
- * Errors: INVALID_ARG, CAPACITY (workspace too small), CUDA.
+ * Errors: INVALID_ARG (also strides of q, keys or values of 2^38 and more), CAPACITY (the workspace is too small, or the work that the sizes
+ * allow does not fit a list of 2^30 entries: kv_heads * n * units of a request * tiles of a table * 3), CUDA.
  */
 int sd_attend(const sd_cache* cache, const sd_rows* rows, const sd_attend_params* params, const void* d_q, void* d_out,
               float* d_lse, void* d_workspace, int64_t workspace_bytes, void* stream);

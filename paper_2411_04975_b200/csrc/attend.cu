@@ -1053,6 +1053,7 @@ int check(const sd_cache* cache, const sd_rows* rows, const sd_attend_params* pr
         if (!sd_stride_ok(prm->q_stride[k]) || !sd_stride_ok(prm->out_stride[k])) return SD_ERR_INVALID_ARG;
     if (prm->q_heads / cache->kv_heads > 128) return SD_ERR_INVALID_ARG;
     if (rows->rows > 1 && prm->q_stride[0] <= 0 || prm->q_heads > 1 && prm->q_stride[1] <= 0) return SD_ERR_INVALID_ARG;
+    if (!sd_out_strides_ok(prm->out_stride, rows->rows, prm->q_heads)) return SD_ERR_INVALID_ARG;
     if (prm->q_stride[0] >= 1ll << 38 || prm->q_stride[1] >= 1ll << 38) return SD_ERR_INVALID_ARG;
     for (int k = 1; k < 4; ++k)                                   // (tiled copies count bytes in 40 bits)
         if (cache->k_stride[k] >= 1ll << 38 || cache->v_stride[k] >= 1ll << 38) return SD_ERR_INVALID_ARG;

@@ -465,6 +465,7 @@ extern "C" int sd_rotate(const sd_cache* cache, const sd_rows* rows, const sd_ro
         if (!d_q || !d_k || !d_v || !d_q_out) return SD_ERR_INVALID_ARG;
         for (const void* p : {d_q, d_k, d_v, (const void*)d_q_out, d_q_weight, d_k_weight})
             if (!sd_aligned(p)) return SD_ERR_INVALID_ARG;
+        if (!sd_out_strides_ok(prm->out_stride, rows->rows, prm->q_heads)) return SD_ERR_INVALID_ARG;
         for (int k = 0; k < 2; ++k)
             if (!sd_stride_ok(prm->q_stride[k]) || !sd_stride_ok(prm->k_stride[k]) || !sd_stride_ok(prm->v_stride[k]) || !sd_stride_ok(prm->out_stride[k]))
                 return SD_ERR_INVALID_ARG;

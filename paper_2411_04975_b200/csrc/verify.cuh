@@ -86,6 +86,8 @@ __device__ __forceinline__ uint4 sd_pack(const float* x) {
 
 // ---- host: arguments -----------------------------------------------------------------------
 inline bool sd_aligned(const void* p) { return ((uintptr_t)p & 15) == 0; }
+// Rows and heads that are written: each has a place of its own.
+inline bool sd_out_strides_ok(const int64_t* s, int rows, int heads) { return (rows <= 1 || s[0] > 0) && (heads <= 1 || s[1] > 0); }
 inline bool sd_stride_ok(long long s) { return s >= 0 && s % 8 == 0; }
 
 // Whether the current device can be given these pointers: the memory `p` lies on is its own (or the host's).

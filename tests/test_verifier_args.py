@@ -48,7 +48,7 @@ def test_attend_refuses(lib, bad):
 
 
 @pytest.mark.parametrize("bad", [dict(q_heads=130), dict(q_heads=258), dict(scale=float("inf")), dict(q_stride=(0, 64)), dict(q_stride=(256, 0)), dict(q_stride=(256, -64)),
-                                 dict(q_stride=(1 << 38, 64))], ids=str)
+                                 dict(q_stride=(1 << 38, 64)), dict(out_stride=(0, 64)), dict(out_stride=(256, 0))], ids=str)
 def test_attend_refuses_heads_and_strides(lib, bad):
     c = cache(kv_heads=1) if bad.get("q_heads") == 130 else cache()
     assert attend(lib, c, rows(), **bad) == -1
