@@ -11,6 +11,21 @@
 // are in flight, one per group: for a unit of up to 128 rows the groups take tiles in turns and join their results at the end, for a larger one each has 128 rows of every tile.
 // While one group is at its softmax the tensor cores work for the other.  Scores and results are in tensor memory; the weights go back over the scores
 // and are read from there.
+//
+// The mathematics: out = sum_p exp(s_p - m) v_p / sum_p exp(s_p - m), s_p = scale * q k_p, in one pass over the places p.  m is a reference that follows the running maximum
+// in steps (a row's sum and result are multiplied by 2^(old - new) only when the maximum has grown by 2^8, so that seldom anything is rescaled and no weight passes 2^8);
+// parts with references of their own, of the two groups or of several blocks, are put together by the logarithms of their sums.  Scores, sums and results have 32 bits;
+// weights are rounded to the type of the values, as the tensor cores want them, and a row's sum adds up the weights as they were before.
+//
+// What bounds it (bf16, 32 query heads on 8 heads of the cache of 128 elements where nothing else is said; microseconds of a call with its joins, and what the bytes or
+// products that it cannot do without would take of that at the measured 6.55 TB/s or 1,625 TFLOP/s):
+//   one token, 8,191 places               19.5   26 %: launches, code fetched for the first time, one chain copy - products - softmax - products, the join
+//   16 requests, 32 .. 400 places         22.5   11 %: the same (fp16, 16 heads of 64, drafts of up to 32)
+//   a draft of 24, 131,072 places        135     61 %: copies in the middle, the same begin and end around it
+//   64 requests, 1,000 .. 8,192 places   350     54 %: tiles of 256 rows take 3,800 cycles (products 2,050 of them; a group's chain of scores, maximum, weights, product
+//                                                is longer than what the other group and the tensor cores need meanwhile), units' ends 12,000 cycles each
+//   128 requests, window of 1,024        200     43 %: units' ends and the two tiles at the window's edges, which take five times as long as whole ones
+//   256 requests, 4,096 places shared    405     26 % of the products: tiles as above, 32-bit planes of both parts and their join (18)
 #include "blackwell.cuh"
 #include "verify.cuh"
 

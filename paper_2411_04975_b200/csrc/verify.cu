@@ -12,7 +12,9 @@ namespace {
 // in which page - is two reads behind one another for all of them.  A row's heads go to the lanes of one or more warps, head_dim / 8 lanes a head and eight
 // elements a lane, always the same eight: what they are multiplied by (cosine, sine and weight in one factor for the element and one for the other of its
 // pair) stays in registers for all heads.  (Factors read from shared memory for every head, and pairs exchanged in 32 bits, took 400
-// instructions for 256 elements and 69 us for 256 requests of up to 65 rows, now 33.)  Bound by the bytes of the rows: every element is read once and written once.
+// instructions for 256 elements and 69 us for 256 requests of up to 65 rows, now 33, 4.3 of the 6.55 TB/s that a
+// copy reaches.)  x' = x w / sqrt(mean(x^2) + eps) has its factor at the end, behind the turn, which is linear: y = (x_a m + x_b o) / sqrt(...).  Bound by the bytes of the
+// rows, every element is read once and written once; one request (5.6 us): by the launch and three reads behind one another.
 constexpr int ROT_THREADS = 128, ROT_WARPS = ROT_THREADS / 32;
 constexpr int ROT_ROWS = 4;
 constexpr int ROT_BATCH = 4;                                      // pieces that a lane has under way
@@ -175,7 +177,8 @@ __global__ void __launch_bounds__(ROT_THREADS, 6) rotate_kernel(const __grid_con
 // ---- sd_accept -----------------------------------------------------------------------------
 // The largest logit of a row, by a block.  The row is cut into chunks of 16 bytes (the first and the last may be shorter: a
 // row starts anywhere); a thread keeps the largest value it has seen and the chunk it was in, and only the winner's chunk is read
-// again for the place.  Bound by reading the logits.
+// again for the place.  Bound by reading the logits: 256 requests' rows of 128,256 bf16 numbers 215 us, 6.8 TB/s (reads alone are faster than a copy); one request 10.6 us, of which
+// 5 are the second launch, which walks the tree.
 constexpr int MAX_THREADS = 512;
 
 template <class T> __device__ __forceinline__ float as_float(T v);
@@ -285,7 +288,7 @@ __global__ void __launch_bounds__(WALK_THREADS) walk_kernel(const WalkArgs a) {
     sd_chain_begin();
     constexpr int WARPS = WALK_THREADS / 32;
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5, blocks = gridDim.x, rank = blockIdx.x;
-    __shared__ long long s_sum[WARPS], s_base, s_block[WALK_BLOCKS];
+    __shared__ long long s_sum[WARPS], s_base, s_first, s_block[WALK_BLOCKS];
     const int part = (a.n + blocks - 1) / blocks, lo_i = min(rank * part, a.n), hi_i = min(lo_i + part, a.n);
     for (int i = lo_i + warp; i < hi_i; i += WARPS) {
         const long long lo = a.offsets[i], hi = a.offsets[i + 1];
@@ -341,6 +344,7 @@ __global__ void __launch_bounds__(WALK_THREADS) walk_kernel(const WalkArgs a) {
         long long before = 0;
         for (int e = 0; e < rank; ++e) before += s_block[e];
         s_base = before;
+        s_first = min(before, (long long)a.rows);
         if (rank == 0) a.new_offsets[0] = 0;
     }
     __syncthreads();
@@ -361,17 +365,16 @@ __global__ void __launch_bounds__(WALK_THREADS) walk_kernel(const WalkArgs a) {
         __syncthreads();
     }
     for (int i = lo_i + warp; i < hi_i; i += WARPS) {
-        const long long lo = a.offsets[i], end = a.new_offsets[i + 1];
-        const int32_t* path = a.path + (long long)i * (a.M + 1);
-        int p[3], kept = 0;
+        const long long lo = a.offsets[i], begin = i == lo_i ? s_first : a.new_offsets[i];   // (what is before the block's first is another block's)
+        const int kept = (int)(a.new_offsets[i + 1] - begin);     // (less than the path where there is no room for it)
+        int32_t* path = a.path + (long long)i * (a.M + 1);
 #pragma unroll
         for (int e = 0; e < 3; ++e) {
-            p[e] = lane + 32 * e <= a.M ? path[lane + 32 * e] : -1;
-            kept += __popc(__ballot_sync(~0u, p[e] >= 0));
+            const int j = lane + 32 * e, p = j <= a.M ? path[j] : -1;
+            if (p < 0) continue;
+            if (j < kept) a.new_tokens[begin + j] = a.targets[lo + p];
+            else path[j] = -1;
         }
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-            if (p[e] >= 0) a.new_tokens[end - kept + lane + 32 * e] = a.targets[lo + p[e]];
     }
     if (rank == blocks - 1)
         for (long long k = s_base + t; k < a.rows; k += WALK_THREADS) a.new_tokens[k] = -1;
@@ -380,7 +383,7 @@ __global__ void __launch_bounds__(WALK_THREADS) walk_kernel(const WalkArgs a) {
 // ---- sd_commit -----------------------------------------------------------------------------
 // A cluster per request, whose blocks take the planes (keys or values of a layer) in turns; a thread per 16 bytes of a line.  Lines only move to smaller
 // places, and a path ascends: what a batch of lines overwrites, no later batch reads.  The new length is written when all blocks have read the old one, which
-// may be the same memory.  Bound by the lines moved (and by the latency of path, table, line).
+// may be the same memory.  Bound by the lines moved: 256 requests, 32 layers, 8 heads of 128: 22.6 us; one request 5.1 us, the launch and path, table and line behind one another.
 constexpr int COMMIT_BATCH = 4, COMMIT_THREADS = 256;
 
 struct CommitArgs {
