@@ -743,7 +743,7 @@ __device__ bool Softmax<T, D>::run(int n) {
                 }
                 mx = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
             }
-            const bool up = mx != -INFINITY && !((mx - top) * scale <= RESCALE);
+            const bool up = row && mx != -INFINITY && !((mx - top) * scale <= RESCALE);
             if (__any_sync(~0u, up)) {
                 const float alpha = up ? ex2((top - mx) * scale) : 1.f;
                 if (up) top = mx;
