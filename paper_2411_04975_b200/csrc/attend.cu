@@ -963,8 +963,8 @@ __device__ void join_row(const AttendArgs& a, const Cut& c, int m, int lane, boo
             for (int k = 0; k < AHEAD; ++k)
                 if (k0 + k < n) {
                     const float* y = a.part + slot(first + k0 + k) * D + lane * E;
-#pragma unroll
-                    for (int e = 0; e < E; e += 2) { const float2 two = *(const float2*)(y + e); z[k][e] = two.x; z[k][e + 1] = two.y; }
+                    if constexpr (E == 4) { const float4 x = *(const float4*)y; z[k][0] = x.x; z[k][1] = x.y; z[k][2] = x.z; z[k][3] = x.w; }
+                    else { const float2 x = *(const float2*)y; z[k][0] = x.x; z[k][1] = x.y; }
                 }
         };
         fetch(0);                                                 // (on their way together with the sums)
