@@ -214,6 +214,8 @@ __device__ __forceinline__ uint32_t largest(const uint4& v, __half) {
 template <class T>
 __global__ void __launch_bounds__(MAX_THREADS) row_max_kernel(const T* logits, long long stride, int vocab, int32_t* targets, int blocks) {
     sd_chain_begin();
+    auto cluster = cooperative_groups::this_cluster();
+    if (blocks > 1) cluster.barrier_arrive();                     // (waited for before the first's memory is written to: it is there by then)
     constexpr int PER = 16 / sizeof(T), AHEAD = 4;
     const int rank = blockIdx.x % blocks, first = rank * MAX_THREADS, step = blocks * MAX_THREADS;
     const long long r = blockIdx.x / blocks;
@@ -256,7 +258,7 @@ __global__ void __launch_bounds__(MAX_THREADS) row_max_kernel(const T* logits, l
         for (int d = MAX_THREADS / 64; d > 0; d >>= 1) all = max(all, __shfl_xor_sync(~0u, all, d));
     }
     if (blocks > 1) {
-        auto cluster = cooperative_groups::this_cluster();
+        cluster.barrier_wait();
         if (t == 0) *cluster.map_shared_rank(&s_block[rank], 0) = all;
         cluster.sync();
         if (rank) return;
@@ -288,6 +290,8 @@ __global__ void __launch_bounds__(WALK_THREADS) walk_kernel(const WalkArgs a) {
     sd_chain_begin();
     constexpr int WARPS = WALK_THREADS / 32;
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5, blocks = gridDim.x, rank = blockIdx.x;
+    auto cluster = cooperative_groups::this_cluster();
+    if (blocks > 1) cluster.barrier_arrive();                     // (waited for before the others' memory is written to: they are there by then)
     __shared__ long long s_sum[WARPS], s_base, s_first, s_block[WALK_BLOCKS];
     const int part = (a.n + blocks - 1) / blocks, lo_i = min(rank * part, a.n), hi_i = min(lo_i + part, a.n);
     for (int i = lo_i + warp; i < hi_i; i += WARPS) {
@@ -332,7 +336,7 @@ __global__ void __launch_bounds__(WALK_THREADS) walk_kernel(const WalkArgs a) {
         for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(~0u, mine, d);
         if (lane == 0) s_sum[warp] = mine;
         __syncthreads();
-        auto cluster = cooperative_groups::this_cluster();
+        cluster.barrier_wait();
         if (t < blocks) {
             mine = 0;
             for (int w = 0; w < WARPS; ++w) mine += s_sum[w];

@@ -1,0 +1,31 @@
+"""Kernels of clusters, by their source: a block's shared memory is reached from another only behind a barrier of the cluster, before which nothing says that it has begun."""
+import os
+import re
+
+import pytest
+
+from paper_2411_04975_b200 import build
+
+BARRIER = re.compile(r"barrier_wait\(\)|cluster\.sync\(\)|cluster_sync\(\)|barrier\.cluster\.wait")
+
+
+def kernels():
+    """(name, body) of the kernels in the sources that reach other blocks' memory."""
+    for f in sorted(os.listdir(build.CSRC)):
+        if f.endswith((".cu", ".cuh")):
+            with open(os.path.join(build.CSRC, f)) as h:
+                parts = re.split(r"__global__", h.read())[1:]
+            for p in parts:
+                body = p.split("\n}\n")[0]
+                if "map_shared_rank" in body:
+                    yield pytest.param(body, id=f + ":" + re.search(r"(\w+_kernel)\(", body).group(1))
+
+
+@pytest.mark.parametrize("body", kernels())
+def test_blocks_of_a_cluster_are_there_before_their_memory_is_reached(body):
+    barrier = BARRIER.search(body)
+    assert barrier and barrier.start() < body.index("map_shared_rank")
+
+
+def test_there_are_such_kernels():
+    assert len(list(kernels())) >= 2

@@ -496,6 +496,19 @@ def test_accept_batches():
     check_accept(empty, np.array([0]), np.zeros((0, 4), dtype=np.int32), np.zeros((0, 4), dtype=np.int32))
 
 
+@pytest.mark.parametrize("n", [15, 16, 17, 18, 23, 31, 32, 33, 64])
+def test_accept_batches_of_a_few_clusters(n):
+    """From 17 requests on the paths are walked by a cluster of eight blocks, of which the last may have none; few rows of a large vocabulary are a cluster each, too."""
+    rng = np.random.default_rng(4100 + n)
+    b = R.Batch([0] * n, rng.integers(-1, 3, n).tolist(), M=3, seed=4100 + n, extra_rows=1, head=64)
+    tokens, want = drafts(b, 70000, rng)
+    logits = torch.randn(b.rows, 70000, generator=torch.Generator().manual_seed(n)).to(BF16)
+    for r, t in want.items():
+        logits[r, t] = 30.0
+    for _ in range(20):
+        check_accept(logits.cuda(), b.offsets, tokens, b.parents)
+
+
 def test_accept_equal_siblings_and_bad_numbers():
     logits = torch.zeros(6, 20, device="cuda:0")
     logits[:, 3] = 1.0
