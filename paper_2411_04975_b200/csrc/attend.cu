@@ -1034,9 +1034,16 @@ __global__ void __launch_bounds__(256) join_planes_kernel(const __grid_constant_
     int i = 0;
     for (int base = 0; base < b.n; base += 256)
         i += __syncthreads_count(base + (int)threadIdx.x < b.n && b.d_offsets[base + threadIdx.x + 1] <= row);
-    if (i >= b.n) return;
-    const Request r = sd_request(b, i, a.c.page_size, a.p.shared);
-    if (row < r.begin || row >= r.begin + r.count) return;
+    auto holds = [&](int request) {
+        if (request >= b.n) return false;
+        const Request r = sd_request(b, request, a.c.page_size, a.p.shared);
+        return row >= r.begin && row < r.begin + r.count;
+    };
+    if (!holds(i)) {                                              // a row of no request, or behind offsets that make no sense: among all
+        bool found = false;
+        for (int at = threadIdx.x; at < b.n; at += 256) found |= holds(at);
+        if (!__syncthreads_or(found)) return;
+    }
     for (int h = threadIdx.x >> 5; h < a.p.q_heads; h += 8) {
         const long long at = row * a.p.q_heads + h;
         const float l0 = a.plane_lse[0][at], l1 = a.plane_lse[1][at];

@@ -1,0 +1,47 @@
+"""Calls in which some requests' numbers make no sense: the others' rows are what they are without them."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2411_04975_b200 as sfx
+import verifier_ref as R
+from test_gpu_verifier import compare
+
+pytestmark = pytest.mark.gpu
+
+FIVE = ([300, 140, 129, 128, 400], [4, 3, 5, 0, 9])               # contexts, drafts: rows 0 .. 4, 5 .. 8, 9 .. 14, 15, 16 .. 25
+
+
+def run(b, offsets=None, table=None, **kw):
+    """(status, out, lse) of a call with these in place of the batch's own."""
+    k, v = b.caches()
+    t, o, cached = b.args()
+    o = o if offsets is None else torch.tensor(offsets, dtype=torch.int64, device="cuda:0")
+    got, lse = torch.full_like(b.q, 7.0, device="cuda:0"), torch.full((b.rows, b.q.shape[1]), 5.0, device="cuda:0")
+    status = torch.full((b.n,), 99, dtype=torch.int32, device="cuda:0")
+    sfx.sd_attend(b.q.cuda(), k, v, t if table is None else table, o, cached, mask=b.mask_arg(), out=got, lse=lse, status=status, **kw)
+    return status.tolist(), got, lse
+
+
+def check_rows(b, requests, got, got_lse):
+    """The rows of these requests against the 64-bit form, which knows nothing of the call's offsets; all others as they were."""
+    out, lse, size = R.attend(b)
+    keep = torch.zeros(b.rows, dtype=torch.bool)
+    for i in requests:
+        keep[int(b.offsets[i]):int(b.offsets[i + 1])] = True
+    compare(b, got[keep], got_lse[keep], out[keep], lse[keep], size[keep])
+    assert (got.cpu()[~keep] == 7.0).all() and (got_lse.cpu()[~keep] == 5.0).all()
+
+
+# offsets, which requests they leave as they are: the others get a status
+BROKEN = [([0, 2 ** 40, 9, 15, 16, 26], (2, 3, 4)), ([0, 5, -3, 15, 16, 26], (0, 3, 4)), ([0, 5, 9, 2 ** 62, 16, 26], (0, 1, 4)), ([2 ** 40, 5, 9, 15, 16, 26], (1, 2, 3, 4)),
+          ([-1, 5, 9, 15, 16, 26], (1, 2, 3, 4))]
+
+
+@pytest.mark.parametrize("offsets,sound", BROKEN, ids=lambda x: str(x[:3]))
+@pytest.mark.parametrize("shared,kw", [(0, {}), (128, {}), (128, dict(shared=128)), (100, dict(shared=100))], ids=str)
+def test_attend_finds_rows_behind_offsets_that_make_no_sense(offsets, sound, shared, kw):
+    b = R.Batch(*FIVE, head=64, page=16, shared=shared, seed=80, extra_rows=2)
+    status, got, lse = run(b, offsets, **kw)
+    assert status == [0 if i in sound else 16 for i in range(5)]
+    check_rows(b, sound, got, lse)
