@@ -121,6 +121,7 @@ struct Rest {                     // of shared memory
     int begun[2];                 // the group has begun its results itself: the first product adds to them
     uint32_t lines[2][4];         // lines of the group's tile with values that are no numbers
     int costs[CHUNKS], all, some; // of the list: chunks of requests, the whole; a request with rows (the prefix is read through its pages)
+    int end;                      // of the requests' rows in the row arrays
     Unit units[UNITS];
     float2 sums[2][128];          // of the groups' rows: reference and sum
 };
@@ -286,19 +287,21 @@ __device__ void add_up(const AttendArgs& a, Rest* s, int t) {
 #pragma unroll 1
     for (int first = t & ~31; first < a.b.n; first += THREADS) {  // (a warp's requests are in one chunk)
         const int i = first + (t & 31);
-        int cost = 0, has = 0x7FFFFFFF;
+        int cost = 0, has = 0x7FFFFFFF, end = 0;
         if (i < a.b.n) {
             const Quote e = quote_of(a, prefix_tiles, i);
             cost = e.cost;
-            if (e.count) has = i;
+            if (e.count) { has = i; end = (int)e.begin + e.count; }
         }
         __syncwarp();
         cost = __reduce_add_sync(~0u, cost);
         has = __reduce_min_sync(~0u, has);
+        end = __reduce_max_sync(~0u, end);
         if ((t & 31) == 0 && cost) {
             atomicAdd(&s->costs[first / size], cost);
             atomicAdd(&s->all, cost);
             atomicMin(&s->some, has);
+            atomicMax(&s->end, end);
         }
     }
 }
@@ -310,12 +313,11 @@ __device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, 
     const sd_rows& b = a.b;
     const int H = a.c.kv_heads, most = 2 * a.tile_rows;           // rows of a unit
     const int prefix_tiles = a.p.window ? 0 : a.p.shared / TILE, sum = s->all, some = s->some;
-    // the prefix, as if it were a request before the others, with all rows
+    // the prefix, as if it were a request before the others, with all rows up to the last of a request (not the last offset, which may make no sense)
     Quote prefix = {0, 0, a.p.shared, 0, 0, prefix_tiles, 0, 0};
     if (prefix_tiles && sum) {
-        const long long rows = b.d_offsets[b.n];
-        prefix.count = rows < 0 ? 0 : (int)min(rows, (long long)b.rows);
-        if (prefix.count) price(prefix, H, a.tile_rows);
+        prefix.count = s->end;
+        price(prefix, H, a.tile_rows);
     }
     const int all = sum + prefix.cost, quota = max((all + (int)gridDim.x - 1) / (int)gridDim.x, LEAST);
     const int lo = (int)min((long long)quota * blockIdx.x, (long long)all), hi = min(lo + quota, all);
@@ -895,7 +897,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (t < CHUNKS) s->costs[t] = 0;
-    if (t == CHUNKS) { s->all = 0; s->some = 0x7FFFFFFF; }
+    if (t == CHUNKS) { s->all = 0; s->some = 0x7FFFFFFF; s->end = 0; }
     if (t == 32 * 3) { bw_prefetch_map(&mk); bw_prefetch_map(&mv); bw_prefetch_map(&mq); }
     if (warp == 1) bw_tmem_alloc(bw_smem(&s->tmem), 512);
     bw_fence_before();

@@ -45,3 +45,13 @@ def test_attend_finds_rows_behind_offsets_that_make_no_sense(offsets, sound, sha
     status, got, lse = run(b, offsets, **kw)
     assert status == [0 if i in sound else 16 for i in range(5)]
     check_rows(b, sound, got, lse)
+
+
+@pytest.mark.parametrize("last", [0, 15, -1, -2 ** 40, 2 ** 40])
+@pytest.mark.parametrize("kw", [{}, dict(shared=128)], ids=str)
+def test_attend_prefix_of_all_sound_rows(last, kw):
+    """The last offset alone makes no sense: the rows before it have their prefix all the same."""
+    b = R.Batch(*FIVE, head=64, page=16, shared=128, seed=81, extra_rows=2)
+    status, got, lse = run(b, b.offsets.tolist()[:-1] + [last], **kw)
+    assert status == [0, 0, 0, 0, 16]
+    check_rows(b, range(4), got, lse)
