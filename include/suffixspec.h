@@ -345,8 +345,10 @@ typedef struct {
     int32_t sinks;                /* ... and always the positions below this          */
     int32_t shared;               /* the first `shared` places of all requests are in */
                                   /* the same pages (one prompt for all): their keys  */
-                                  /* are read once for the batch.  0 .. every         */
-                                  /* d_cached[i] of a request with rows               */
+                                  /* are read once for the batch, through the table   */
+                                  /* of the first request with rows; a page of these  */
+                                  /* outside the cache is told to all requests with   */
+                                  /* rows.  0 .. every d_cached[i] of such a request  */
     int64_t q_stride[2], out_stride[2];     /* elements from row to row, head to head: multiples of 8, > 0 where there is more than one */
 } sd_attend_params;
 

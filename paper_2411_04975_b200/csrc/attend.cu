@@ -429,9 +429,15 @@ __device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, 
     }
 }
 
-// Pages that a request's rows see: told where one is none of the cache's.
-__device__ void write_status(const AttendArgs& a, int lane) {
+// Pages that a request's rows see: told where one is none of the cache's.  (A shared prefix is read through the pages of one request: all rows see those.)
+__device__ void write_status(const AttendArgs& a, const Rest* s, int lane) {
     const sd_rows& b = a.b;
+    const int prefix_places = a.p.window ? 0 : a.p.shared / TILE * TILE;
+    bool prefix = false;
+    if (s->some < b.n) {
+#pragma unroll 1
+        for (int e = lane; e < (prefix_places + a.c.page_size - 1) / a.c.page_size; e += 32) prefix |= sd_page(b, a.c.n_pages, s->some, e) < 0;
+    }
 #pragma unroll 1
     for (int i = blockIdx.x; i < b.n; i += gridDim.x) {
         const Request r = sd_request(b, i, a.c.page_size, a.p.shared);
@@ -439,7 +445,7 @@ __device__ void write_status(const AttendArgs& a, int lane) {
         if (r.count) {
             const int P = a.c.page_size, from = a.p.window ? max(0, r.cached - a.p.window + 1) : 0;
             const int sinks = a.p.window ? min(min(a.p.sinks, r.cached), from) : 0;
-            bool bad = false;
+            bool bad = prefix;
 #pragma unroll 1
             for (int e = lane; e < (sinks + P - 1) / P; e += 32) bad |= sd_page(b, a.c.n_pages, i, e) < 0;
 #pragma unroll 1
@@ -912,7 +918,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
         if (warp == 0) walk_units<D>(a, &mq, s, q, f, lane);
         else {
             copy_values<D>(f);
-            if (a.b.d_status) write_status(a, lane);
+            if (a.b.d_status) write_status(a, s, lane);
         }
     }
     else if (warp == 1 || warp == 3) {

@@ -55,3 +55,20 @@ def test_attend_prefix_of_all_sound_rows(last, kw):
     status, got, lse = run(b, b.offsets.tolist()[:-1] + [last], **kw)
     assert status == [0, 0, 0, 0, 16]
     check_rows(b, range(4), got, lse)
+
+
+@pytest.mark.parametrize("value", [-1, 2 ** 31 - 1])
+@pytest.mark.parametrize("idle", [False, True])
+def test_attend_bad_page_in_a_shared_prefix_is_told_to_all(value, idle):
+    """The prefix is read through one request's pages: where one of them is none of the cache's, no request's rows are of use."""
+    b = R.Batch(FIVE[0], ([-1] if idle else [4]) + FIVE[1][1:], head=64, page=16, shared=128, seed=82)
+    k, v = b.caches()
+    table, offsets, cached = b.args()
+    first = 1 if idle else 0
+    table[first, 3] = value
+    status = torch.full((5,), 99, dtype=torch.int32, device="cuda:0")
+    sfx.sd_attend(b.q.cuda(), k, v, table, offsets, cached, mask=b.mask_arg(), status=status, shared=128)
+    assert status.tolist() == [0 if idle else 32, 32, 32, 32, 32]
+    status.fill_(99)
+    sfx.sd_attend(b.q.cuda(), k, v, table, offsets, cached, mask=b.mask_arg(), status=status, shared=128, window=500)     # (each reads its own)
+    assert status.tolist() == [32 if i == first else 0 for i in range(5)]
