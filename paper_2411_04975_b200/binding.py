@@ -188,7 +188,7 @@ class _PlainCall:
         heads, D = _q_heads(q), k_cache.shape[-1]
         if heads > 65536 or freq.numel() > 64:
             raise TypeError("rotate: at most 65,536 heads and 64 frequencies")
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        out = torch.empty(q.shape, dtype=q.dtype, device=_device()) if out is None else out
         strides = [_heads(t, dt, (rows, h, D), name) for t, h, name in ((q, heads, "q"), (k, cache.kv_heads, "k"), (v, cache.kv_heads, "v"), (out, heads, "out"))]
         p = _RotateParams(heads, 2 * freq.numel(), int(interleaved), scale, eps, *strides)
         return self._lib.sd_rotate(
@@ -204,14 +204,14 @@ class _PlainCall:
         for name, x in (("q_heads", heads), ("window", window), ("sinks", sinks), ("shared", shared)):
             if not 0 <= x <= (65536 if name == "q_heads" else 0x7FFFFFFF):
                 raise SuffixSpecError(-1, f"sd_attend: {name} {x}")
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        out = torch.empty(q.shape, dtype=q.dtype, device=_device()) if out is None else out
         scale = max(D, 1) ** -0.5 if scale is None else scale
         p = _AttendParams(heads, scale, window, sinks, shared, _heads(q, dt, (rows, heads, D), "q"), _heads(out, dt, (rows, heads, D), "out"))
         lse = _array(lse, torch.float32, (rows, heads), "lse")
         size = self._lib.sd_attend_workspace(C.byref(cache), C.byref(b), C.byref(p))
         if size < 0:
             return size
-        work = torch.empty(size, dtype=torch.uint8, device=q.device)
+        work = torch.empty(size, dtype=torch.uint8, device=_device())
         return self._lib.sd_attend(C.byref(cache), C.byref(b), C.byref(p), q.data_ptr(), out.data_ptr(), lse, work.data_ptr(), size, _stream()) or out
 
     def accept(self, logits, offsets, tokens, parents, out, status):
@@ -222,9 +222,9 @@ class _PlainCall:
             raise TypeError(f"accept: logits of {logits.dtype}, drafts of {M}")
         _here(logits, "logits")
         if out is None:
-            i32 = dict(dtype=torch.int32, device=logits.device)
+            i32 = dict(dtype=torch.int32, device=_device())
             out = {"targets": torch.empty(rows, **i32), "path": torch.empty(n, M + 1, **i32),
-                   "offsets": torch.empty(n + 1, dtype=torch.int64, device=logits.device), "tokens": torch.empty(rows, **i32)}
+                   "offsets": torch.empty(n + 1, dtype=torch.int64, device=_device()), "tokens": torch.empty(rows, **i32)}
         targets, path, new_offsets, new_tokens = (out[k] for k in ("targets", "path", "offsets", "tokens"))
         args = [_array(t, dt, shape, name) for t, dt, shape, name in (
             (offsets, torch.int64, (n + 1,), "offsets"), (tokens, torch.int32, (n, M), "tokens"), (parents, torch.int32, (n, M), "parents"),
@@ -239,9 +239,14 @@ class _PlainCall:
         n, M1 = path.shape
         b = _Rows(n, 0, M1 - 1, table.shape[1], None, _array(cached, torch.int32, (n,), "cached"),
                   _array(table, torch.int32, (n, table.shape[1]), "table"), None, _array(status, torch.int32, (n,), "status"))
-        out = torch.empty(cached.shape, dtype=cached.dtype, device=cached.device) if out is None else out
+        out = torch.empty(cached.shape, dtype=cached.dtype, device=_device()) if out is None else out
         return self._lib.sd_commit(C.byref(cache), C.byref(b), _array(path, torch.int32, (n, M1), "path"),
                                    _array(out, torch.int32, (n,), "out"), _stream()) or out
+
+
+def _device() -> torch.device:
+    """Where results and workspaces are made: the arguments may be in pinned host memory."""
+    return torch.device("cuda", _current_device())
 
 
 def _here(t: torch.Tensor, name: str) -> None:

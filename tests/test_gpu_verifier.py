@@ -694,6 +694,22 @@ def test_calls_through_ctypes_alone(monkeypatch):
     check_commit(R.Batch([20, 30], [10, 10], M=10, seed=63, layers=2), [[0, 4], [0]])
 
 
+def test_small_arrays_in_pinned_memory():
+    """What says where rows and pages are, and what is told of them, in pinned host memory; queries, keys, values and results on the device."""
+    b = R.Batch([200, 31, 700], [6, 9, 64], head=128, seed=65, shared=16)
+    pin = lambda t: t.cpu().pin_memory()                          # noqa: E731
+    table, offsets, cached = (pin(t) for t in b.args())
+    k, v = b.caches()
+    lse, status = torch.zeros(b.rows, 4).pin_memory(), torch.full((3,), 99, dtype=torch.int32).pin_memory()
+    got = sfx.sd_attend(b.q.cuda(), k, v, table, offsets, cached, mask=pin(b.mask_arg()), lse=lse, status=status)
+    torch.cuda.synchronize()
+    assert got.is_cuda and status.tolist() == [0, 0, 0]
+    compare(b, got, lse, *R.attend(b))
+    freq = torch.zeros(32, dtype=torch.float64).pin_memory()
+    got = sfx.sd_rotate(b.q.cuda(), b.k.cuda(), b.v.cuda(), k, v, table, offsets, cached, freq, mask=pin(b.mask_arg()))
+    assert got.is_cuda and torch.equal(got.cpu(), b.q)
+
+
 def test_no_requests():
     b = R.Batch([3], [2], seed=64)
     k, v = b.caches()

@@ -110,3 +110,51 @@ def test_plain_calls_take_the_same_arguments():
         n = len(inspect.signature(getattr(binding._PlainCall(binding._lib), name)).parameters)
         with pytest.raises(TypeError, match=f"{n} arguments expected"):
             getattr(native, name)()
+
+
+class _Library:
+    """Takes every call; what it was given as the workspace of sd_attend is kept."""
+
+    def sd_attend_workspace(self, *a):
+        return 1 << 20
+
+    def sd_attend(self, *a):
+        self.work = a[6]
+        return 0
+
+    def sd_rotate(self, *a):
+        return 0
+
+    sd_accept = sd_commit = sd_rotate
+
+
+def test_results_and_workspaces_are_on_the_device_for_arguments_in_host_memory(monkeypatch):
+    """Tensors in pinned host memory are taken; what the call makes itself has to be the device's all the same: pageable memory is not for its kernels."""
+    import torch
+    made, empty = [], torch.empty
+
+    def record(*a, device=None, **kw):
+        made.append(torch.device(device))
+        return empty(*a, **kw)
+
+    for name, f in (("_here", lambda t, name: None), ("_ptr", lambda t, dtype, name: None if t is None else t.data_ptr()), ("_stream", lambda: 0), ("_current_device", lambda: 0)):
+        monkeypatch.setattr(binding, name, f)
+    monkeypatch.setattr(binding.torch, "empty", record)
+    lib = _Library()
+    call = binding._PlainCall(lib)
+    q, k = torch.zeros(3, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16)
+    rows = torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    table, cached = torch.zeros(1, 2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    offsets = torch.zeros(2, dtype=torch.int64)
+    call.rotate(q, rows, rows, k, k, table, offsets, cached, torch.zeros(32, dtype=torch.float64), None, None, None, None, 1e-6, False, 1.0, None, None)
+    assert len(made) == 1
+    call.attend(q, k, k, table, offsets, cached, None, None, 0, 0, 0, None, None, None)
+    assert len(made) == 3 and lib.work
+    call.attend(q, k, k, table, offsets, cached, None, None, 0, 0, 0, q, None, None)
+    assert len(made) == 4
+    draft = torch.zeros(1, 3, dtype=torch.int32)
+    call.accept(torch.zeros(3, 9), offsets, draft, draft, None, None)
+    assert len(made) == 8
+    call.commit(k, k, table, cached, torch.zeros(1, 4, dtype=torch.int32), None, None)
+    assert len(made) == 9
+    assert all(d == torch.device("cuda", 0) for d in made)
