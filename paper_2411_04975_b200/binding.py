@@ -237,6 +237,7 @@ class _PlainCall:
         if path.dim() != 2 or not 1 <= path.shape[1] <= MAX_DRAFT + 1 or table.dim() != 2:
             raise TypeError("commit: expected a path [n, max_draft + 1] and a table [n, pages]")
         n, M1 = path.shape
+        _counts("path, table", n, table.shape[1])
         b = _Rows(n, 0, M1 - 1, table.shape[1], None, _array(cached, torch.int32, (n,), "cached"),
                   _array(table, torch.int32, (n, table.shape[1]), "table"), None, _array(status, torch.int32, (n,), "status"))
         out = torch.empty(cached.shape, dtype=cached.dtype, device=_device()) if out is None else out
@@ -261,6 +262,12 @@ def _array(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, name: st
     if t is not None:
         _here(t, name)
     return p
+
+
+def _counts(name: str, *sizes: int) -> None:
+    """Sizes that the structures hold in 31 bits (a larger one would go over as what is left of it)."""
+    if max(sizes) > 0x7FFFFFFE:
+        raise TypeError(f"{name}: a size of {max(sizes)} is beyond 31 bits")
 
 
 def _length(t: torch.Tensor, name: str) -> int:
@@ -289,6 +296,7 @@ def _cache_of(k: torch.Tensor, v: torch.Tensor, dims: tuple) -> _Cache:
                         f"that) with adjacent elements, got {k.dtype} {tuple(k.shape)} and {v.dtype} {tuple(v.shape)}")
     _here(k, "k_cache")
     _here(v, "v_cache")
+    _counts("k_cache, v_cache", *k.shape)
     layers = k.dim() == 5
     st = [(C.c_int64 * 4)(t.stride(0) if layers else 0, t.stride(-4), t.stride(-3), t.stride(-2)) for t in (k, v)]
     return _Cache(k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], k.shape[-2], k.shape[-1], k.shape[0] if layers else 1, k.shape[-4], k.shape[-3], *st)
@@ -298,6 +306,7 @@ def _rows_of(rows: int, table, offsets, cached, mask, status) -> _Rows:
     n = _length(offsets, "offsets") - 1
     if n < 0 or table.dim() != 2:
         raise TypeError("offsets: expected one more than requests; table: expected [n, pages]")
+    _counts("rows, offsets, table", rows, n, table.shape[1])
     M = MAX_DRAFT
     if mask is not None:
         if mask.dim() != 3 or mask.shape[1] > MAX_DRAFT:

@@ -158,3 +158,32 @@ def test_results_and_workspaces_are_on_the_device_for_arguments_in_host_memory(m
     call.commit(k, k, table, cached, torch.zeros(1, 4, dtype=torch.int32), None, None)
     assert len(made) == 9
     assert all(d == torch.device("cuda", 0) for d in made)
+
+
+@pytest.mark.parametrize("size", [2 ** 31, 2 ** 32 + 3])
+def test_sizes_beyond_31_bits_are_refused(monkeypatch, size):
+    """ctypes keeps the low bits of a number that its field has no room for."""
+    import torch
+    monkeypatch.setattr(binding, "_here", lambda t, name: None)
+    monkeypatch.setattr(binding, "_ptr", lambda t, dtype, name: None if t is None else t.data_ptr())
+    monkeypatch.setattr(binding, "_stream", lambda: 0)
+    monkeypatch.setattr(binding, "_device", lambda: torch.device("cpu"))
+    call = binding._PlainCall(_Library())
+    table, cached, offsets = torch.zeros(1, 2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int64)
+    q, k = torch.zeros(1, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16)
+    rows, freq = torch.zeros(1, 2, 64, dtype=torch.bfloat16).expand(size, 2, 64), torch.zeros(32, dtype=torch.float64)
+    many, path = q.expand(size, 4, 64), torch.zeros(1, 4, dtype=torch.int32)
+    wide = table[:, :1].expand(1, size)
+
+    def attend(q=q, k=k, table=table):
+        return call.attend(q, k, k, table, offsets, cached, None, None, 0, 0, 0, q, None, None)
+
+    assert attend() is q
+    for kw in (dict(q=many), dict(table=wide), dict(k=k[:1].expand(size, 16, 2, 64)), dict(k=k[:, :1].expand(2, size, 2, 64))):
+        with pytest.raises(TypeError, match="beyond 31 bits"):
+            attend(**kw)
+    with pytest.raises(TypeError, match="beyond 31 bits"):
+        call.rotate(many, rows, rows, k, k, table, offsets, cached, freq, None, None, None, None, 1e-6, False, 1.0, many, None)
+    for kw in (dict(table=wide), dict(k=k[None].expand(size, 2, 16, 2, 64))):
+        with pytest.raises(TypeError, match="beyond 31 bits"):
+            call.commit(kw.get("k", k), kw.get("k", k), kw.get("table", table), cached, path, cached, None)
