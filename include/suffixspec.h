@@ -492,6 +492,12 @@ void sd_debug_fail_alloc(int64_t k);
  */
 void sd_debug_small_clusters(int32_t on);
 
+/*
+ * sd_debug_attend_limit: test hook for waits that are given up.  From now on (cycles > 0) the kernel of sd_attend gives up a wait on the device that takes longer than
+ * so many cycles, where it otherwise does after 4e9; cycles = 0 switches it off.
+ */
+void sd_debug_attend_limit(int64_t cycles);
+
 #ifdef __cplusplus
 }
 #endif

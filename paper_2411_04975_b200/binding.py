@@ -26,7 +26,7 @@ STATUS_BAD_ROWS, STATUS_BAD_PAGE = 16, 32
 
 EXPORTS = ["sd_build", "sd_build_requests", "sd_append", "sd_speculate", "sd_step", "sd_speculate_noalloc", "sd_query_counts",
            "sd_enumerate", "sd_slot_info", "sd_entropy", "sd_stats", "sd_free", "sd_trim", "sd_strerror", "sd_debug_fail_alloc",
-           "sd_debug_small_clusters", "sd_rotate", "sd_attend", "sd_attend_workspace", "sd_accept", "sd_commit"]
+           "sd_debug_small_clusters", "sd_debug_attend_limit", "sd_rotate", "sd_attend", "sd_attend_workspace", "sd_accept", "sd_commit"]
 
 
 class SuffixSpecError(RuntimeError):
@@ -120,6 +120,8 @@ def library() -> C.CDLL:
         lib.sd_debug_fail_alloc.argtypes = [C.c_int64]
         lib.sd_debug_small_clusters.restype = None
         lib.sd_debug_small_clusters.argtypes = [C.c_int32]
+        lib.sd_debug_attend_limit.restype = None
+        lib.sd_debug_attend_limit.argtypes = [C.c_int64]
         cache, rows = C.POINTER(_Cache), C.POINTER(_Rows)
         lib.sd_rotate.restype = C.c_int
         lib.sd_rotate.argtypes = [cache, rows, C.POINTER(_RotateParams)] + [vp] * 9

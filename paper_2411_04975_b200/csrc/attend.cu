@@ -30,6 +30,7 @@
 #include "verify.cuh"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 namespace {
@@ -60,6 +61,7 @@ struct AttendArgs {
     float* lse;
     int group, tile_rows;         // query heads that share a head of the cache; rows whose heads make a tile's packed rows
     float scale;                  // of scores, for powers of two; not negative: the products turn the sign
+    long long limit;              // cycles that a wait may take
     int box;                      // lines that one copy fetches
     Cut* cuts;                    // [grid]: the unit that begins in block c and is cut
     float* part;                  // [2 * grid][256][D]: packed rows of a cut unit; slot 2c: it came from the block before, 2c + 1: it goes on in the next
@@ -117,7 +119,7 @@ struct Shape {
 struct Rest {                     // of shared memory
     uint64_t full[16], empty[16], s_full[2], p_ready[2], o_done[2], q_full[2], q_empty[2], unit_full[UNITS], unit_empty[UNITS], meet, group_meet[2], over[2], lead;
     uint32_t tmem;
-    int stop;
+    Waits waits;
     int begun[2];                 // the group has begun its results itself: the first product adds to them
     uint32_t lines[2][4];         // lines of the group's tile with values that are no numbers
     int costs[CHUNKS], all, some; // of the list: chunks of requests, the whole; a request with rows (the prefix is read through its pages)
@@ -175,12 +177,52 @@ __device__ __noinline__ Sight sight_of(const sd_rows& b, int request, int cached
 template <class T> struct IsBf16 { static constexpr bool v = false; };
 template <> struct IsBf16<__nv_bfloat16> { static constexpr bool v = true; };
 
-// Given up: the copies in flight come to their end.
+// Each warp is through with its part: has any given up?  Then nobody asks for more now, and what was asked for comes to its end (of warps too that were through before).
+__device__ __forceinline__ bool all_through(Rest* s) {
+    __syncwarp();
+    bw_fence_before();
+    asm volatile("barrier.cta.sync 1, %0;" ::"n"(THREADS) : "memory");
+    return s->waits.stop;
+}
+
+// Given up: the copies in flight come to their end: of queries, and those of lines that a warp has copied, up to slot `it`.
 __device__ __noinline__ void drain(uint64_t* full, uint32_t slots, uint32_t filled) {
     for (uint32_t e = 0; e < slots && e < filled; ++e) {
         const uint32_t last = (filled - 1 - e) / slots * slots + e;
-        int never = 0;
-        bw_wait_slow(bw_smem(&full[e]), (last / slots) & 1, &never, 200000000ll);
+        bw_wait_end(bw_smem(&full[e]), (last / slots) & 1);
+    }
+}
+
+template <int D>
+__device__ __noinline__ void drain_lines(Rest* s, uint32_t it) {
+    constexpr uint32_t BARS = Shape<D>::BARS;
+    for (uint32_t k = it >= BARS ? it - BARS : it % 2; k < it; k += 2) bw_wait_end(bw_smem(&s->full[k % BARS]), (k / BARS) & 1);
+}
+
+// Pages that a request's rows see: told where one is none of the cache's.  (A shared prefix is read through the pages of one request: all rows see those.)
+__device__ __noinline__ void write_status(const AttendArgs& a, const Rest* s, int lane) {
+    const sd_rows& b = a.b;
+    const int prefix_places = a.p.window ? 0 : a.p.shared / TILE * TILE;
+    bool prefix = false;
+    if (s->some < b.n) {
+#pragma unroll 1
+        for (int e = lane; e < (prefix_places + a.c.page_size - 1) / a.c.page_size; e += 32) prefix |= sd_page(b, a.c.n_pages, s->some, e) < 0;
+    }
+#pragma unroll 1
+    for (int i = blockIdx.x; i < b.n; i += gridDim.x) {
+        const Request r = sd_request(b, i, a.c.page_size, a.p.shared);
+        int st = r.status;
+        if (r.count) {
+            const int P = a.c.page_size, from = a.p.window ? max(0, r.cached - a.p.window + 1) : 0;
+            const int sinks = a.p.window ? min(min(a.p.sinks, r.cached), from) : 0;
+            bool bad = prefix;
+#pragma unroll 1
+            for (int e = lane; e < (sinks + P - 1) / P; e += 32) bad |= sd_page(b, a.c.n_pages, i, e) < 0;
+#pragma unroll 1
+            for (int e = from / P + lane; e <= (r.cached + r.count - 1) / P; e += 32) bad |= sd_page(b, a.c.n_pages, i, e) < 0;
+            if (__any_sync(~0u, bad)) st |= SD_STATUS_BAD_PAGE;
+        }
+        if (lane == 0) b.d_status[i] = st;
     }
 }
 
@@ -212,7 +254,7 @@ struct Lines {
     __device__ __forceinline__ bool copy(const Unit& u, int k, bool wide) {
         const uint32_t e = it % S::SLOTS, bar = bw_smem(&s->full[it % S::BARS]), before = it - S::SLOTS;
         const int boxes = __popc(__ballot_sync(~0u, here));
-        if (it >= S::SLOTS && !bw_wait_warp(bw_smem(&s->empty[before % S::BARS]), (before / S::BARS) & 1, &s->stop)) return false;
+        if (it >= S::SLOTS && !bw_wait_warp(bw_smem(&s->empty[before % S::BARS]), (before / S::BARS) & 1, &s->waits)) return false;
         if ((threadIdx.x & 31) == 0) {
             if (!wide) bw_arrive(bw_smem(&s->empty[it % S::BARS]));          // (for the group that does not use it)
             bw_arrive_expect(bar, boxes * a.box * 128);
@@ -226,21 +268,14 @@ struct Lines {
         it += 2;
         return true;
     }
-    // Given up: this warp's copies in flight come to their end.
-    __device__ __noinline__ void drain() {
-        for (uint32_t k = it >= S::BARS ? it - S::BARS : v; k < it; k += 2) {
-            int never = 0;
-            bw_wait_slow(bw_smem(&s->full[k % S::BARS]), (k / S::BARS) & 1, &never, 200000000ll);
-        }
-    }
 };
 
 template <int D>
 __device__ void copy_values(Lines<D> f) {
     for (int n = 0;; ++n) {
-        if (!bw_wait_warp(bw_smem(&f.s->unit_full[n % UNITS]), (n / UNITS) & 1, &f.s->stop)) break;
+        if (!bw_wait_warp(bw_smem(&f.s->unit_full[n % UNITS]), (n / UNITS) & 1, &f.s->waits)) break;
         const Unit& u = f.s->units[n % UNITS];
-        if (u.kind == DONE) return;
+        if (u.kind == DONE) break;
         const bool wide = u.rows > f.a.tile_rows;
         const int k1 = u.k1;
         bool ok = true;
@@ -250,7 +285,8 @@ __device__ void copy_values(Lines<D> f) {
         if (!ok) break;
         bw_arrive_warp(bw_smem(&f.s->unit_empty[n % UNITS]));
     }
-    f.drain();
+    if (f.a.b.d_status) write_status(f.a, f.s, threadIdx.x & 31);
+    if (all_through(f.s)) drain_lines<D>(f.s, f.it);
 }
 
 // ---- the list's walker ---------------------------------------------------------------------
@@ -389,7 +425,7 @@ __device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, 
                     cut.rows = u.rows; cut.head = u.head; cut.prefix = first < 0; cut.begin = u.begin;
                 }
                 const int place = at % UNITS;
-                ok = at < UNITS || bw_wait_warp(bw_smem(&s->unit_empty[place]), (at / UNITS - 1) & 1, &s->stop);
+                ok = at < UNITS || bw_wait_warp(bw_smem(&s->unit_empty[place]), (at / UNITS - 1) & 1, &s->waits);
                 if (!ok) break;
                 if (lane == 0) {
                     s->units[place] = u;
@@ -403,10 +439,12 @@ __device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, 
                     if (k > u.k0) continue;
                     // its queries: a tile's rows and heads in one copy for each half of the head; rows behind the unit's come along and are left alone
 #pragma unroll 1
-                    for (int row = 0; row < u.rows && ok; row += a.tile_rows, ++qi) {
+                    for (int row = 0; row < u.rows; row += a.tile_rows) {
                         const uint32_t slot = qi % 2, bar = bw_smem(&s->q_full[slot]);
-                        ok = qi < 2 || bw_wait_warp(bw_smem(&s->q_empty[slot]), (qi / 2 - 1) & 1, &s->stop);
-                        if (!ok || lane) continue;
+                        ok = qi < 2 || bw_wait_warp(bw_smem(&s->q_empty[slot]), (qi / 2 - 1) & 1, &s->waits);
+                        if (!ok) break;
+                        ++qi;                                     // (counted when it is asked for: drain() looks for the last of each slot)
+                        if (lane) continue;
                         bw_arrive_expect(bar, S::HALVES * 128 * a.group * a.tile_rows);
 #pragma unroll 1
                         for (int h = 0; h < S::HALVES; ++h) bw_load_3d(q + slot * S::Q_BYTES + h * S::HALF_BYTES, mq, h * 64, u.head * a.group, (int)u.begin + row, bar);
@@ -419,69 +457,41 @@ __device__ void walk_units(const AttendArgs& a, const CUtensorMap* mq, Rest* s, 
     }
     if (lane == 0) a.cuts[blockIdx.x] = cut;
     const int e = at % UNITS;
-    if (ok && (at < UNITS || bw_wait_warp(bw_smem(&s->unit_empty[e]), (at / UNITS - 1) & 1, &s->stop)) && lane == 0) {
+    if (ok && (at < UNITS || bw_wait_warp(bw_smem(&s->unit_empty[e]), (at / UNITS - 1) & 1, &s->waits)) && lane == 0) {
         s->units[e].kind = DONE;
         bw_arrive(bw_smem(&s->unit_full[e]));
     }
-    if (!ok) {
+    if (all_through(s)) {
         drain(s->q_full, 2, qi);
-        keys.drain();
-    }
-}
-
-// Pages that a request's rows see: told where one is none of the cache's.  (A shared prefix is read through the pages of one request: all rows see those.)
-__device__ void write_status(const AttendArgs& a, const Rest* s, int lane) {
-    const sd_rows& b = a.b;
-    const int prefix_places = a.p.window ? 0 : a.p.shared / TILE * TILE;
-    bool prefix = false;
-    if (s->some < b.n) {
-#pragma unroll 1
-        for (int e = lane; e < (prefix_places + a.c.page_size - 1) / a.c.page_size; e += 32) prefix |= sd_page(b, a.c.n_pages, s->some, e) < 0;
-    }
-#pragma unroll 1
-    for (int i = blockIdx.x; i < b.n; i += gridDim.x) {
-        const Request r = sd_request(b, i, a.c.page_size, a.p.shared);
-        int st = r.status;
-        if (r.count) {
-            const int P = a.c.page_size, from = a.p.window ? max(0, r.cached - a.p.window + 1) : 0;
-            const int sinks = a.p.window ? min(min(a.p.sinks, r.cached), from) : 0;
-            bool bad = prefix;
-#pragma unroll 1
-            for (int e = lane; e < (sinks + P - 1) / P; e += 32) bad |= sd_page(b, a.c.n_pages, i, e) < 0;
-#pragma unroll 1
-            for (int e = from / P + lane; e <= (r.cached + r.count - 1) / P; e += 32) bad |= sd_page(b, a.c.n_pages, i, e) < 0;
-            if (__any_sync(~0u, bad)) st |= SD_STATUS_BAD_PAGE;
-        }
-        if (lane == 0) b.d_status[i] = st;
+        drain_lines<D>(s, keys.it);
     }
 }
 
 // ---- products ------------------------------------------------------------------------------
-// (A warp for each group: to wait, to issue and to commit takes it as long as the products take.)  False: given up.
+// (A warp for each group: to wait, to issue and to commit takes it as long as the products take.)  `leader`: the lane that issues.
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(~0u, x, 0); }   // (the same in all lanes, and known to be)
 
 template <class T, int D>
-__device__ bool multiply(const AttendArgs& a, Rest* s, uint32_t ring, uint32_t q, uint32_t tmem_, int w) {
+__device__ void multiply(const AttendArgs& a, Rest* s, uint32_t ring, uint32_t q, uint32_t tmem_, int w, bool leader) {
     using S = Shape<D>;
     const uint32_t qk = bw_idesc(IsBf16<T>::v, 128, TILE, false) | (a.p.scale < 0.f ? 1u << 13 : 0u);   // (negated queries)
     constexpr uint32_t pv = bw_idesc(IsBf16<T>::v, 128, D, true);
     const uint32_t tmem = uniform(tmem_), S0 = tmem + w * TILE, O0 = tmem + 2 * TILE + w * TILE;
-    const bool leader = bw_elect();
     uint32_t it = 0, qi = 0, count = 0, wides = 0;                // slots, queries, jobs, wide units behind
     for (int n = 0;; ++n) {
-        if (!bw_wait_warp(bw_smem(&s->unit_full[n % UNITS]), (n / UNITS) & 1, &s->stop)) return false;
+        if (!bw_wait_warp(bw_smem(&s->unit_full[n % UNITS]), (n / UNITS) & 1, &s->waits)) return;
         const Unit& u = s->units[n % UNITS];
         const int kind = uniform(u.kind), tiles = uniform(u.k1 - u.k0);
         const bool wide = uniform(u.rows) > a.tile_rows;
         bw_arrive_warp(bw_smem(&s->unit_empty[n % UNITS]));
-        if (kind == DONE) return true;
+        if (kind == DONE) return;
         const int step = wide ? 1 : 2, first = wide ? 0 : w;      // the group's tiles
         const uint32_t mine = (qi + (wide ? w : 0)) % 2;          // its queries
         // Of a wide unit the second group begins when the first is halfway through its first tile: from then on the one computes while the other's products run.
-        if (wide && w && !bw_wait_warp(bw_smem(&s->lead), wides++ & 1, &s->stop)) return false;
+        if (wide && w && !bw_wait_warp(bw_smem(&s->lead), wides++ & 1, &s->waits)) return;
         for (int k = 0; k < (wide ? 2 : 1); ++k) {
             const uint32_t e = (qi + k) % 2;
-            if (!bw_wait_warp(bw_smem(&s->q_full[e]), ((qi + k) / 2) & 1, &s->stop)) return false;
+            if (!bw_wait_warp(bw_smem(&s->q_full[e]), ((qi + k) / 2) & 1, &s->waits)) return;
             if (e != mine || first >= tiles) bw_arrive_warp(bw_smem(&s->q_empty[e]));   // (not used by this group)
         }
 #pragma unroll 1
@@ -489,8 +499,8 @@ __device__ bool multiply(const AttendArgs& a, Rest* s, uint32_t ring, uint32_t q
             const int next = j + step;
             const uint32_t v = it + 2 * j + 1, k = it + 2 * next;
             if (j >= 0) {
-                if (!bw_wait_warp(bw_smem(&s->full[v % S::BARS]), (v / S::BARS) & 1, &s->stop)) return false;
-                if (!bw_wait_warp(bw_smem(&s->p_ready[w]), count++ & 1, &s->stop)) return false;
+                if (!bw_wait_warp(bw_smem(&s->full[v % S::BARS]), (v / S::BARS) & 1, &s->waits)) return;
+                if (!bw_wait_warp(bw_smem(&s->p_ready[w]), count++ & 1, &s->waits)) return;
                 bw_fence_after();
                 const bool add = j >= step || uniform(*(volatile int*)&s->begun[w]);
                 const uint64_t vd = bw_desc_across(ring + v % S::SLOTS * S::SLOT_BYTES, S::HALF_BYTES);
@@ -498,7 +508,7 @@ __device__ bool multiply(const AttendArgs& a, Rest* s, uint32_t ring, uint32_t q
                 for (int i = 0; i < TILE / 16; ++i) bw_mma_ts(O0, S0 + i * 8, vd + (i * 2048 >> 4), pv, add || i > 0, leader);
             }
             if (next < tiles) {
-                if (!bw_wait_warp(bw_smem(&s->full[k % S::BARS]), (k / S::BARS) & 1, &s->stop)) return false;
+                if (!bw_wait_warp(bw_smem(&s->full[k % S::BARS]), (k / S::BARS) & 1, &s->waits)) return;
                 bw_fence_after();
                 const uint64_t qd = bw_desc(q + mine * S::Q_BYTES), kd = bw_desc(ring + k % S::SLOTS * S::SLOT_BYTES);
 #pragma unroll
@@ -568,7 +578,7 @@ struct Softmax {
     __device__ __forceinline__ bool meet_of(bool both) {
         const uint32_t bar = bw_smem(both ? &s->meet : &s->group_meet[w]), parity = (both ? meets++ : group_meets++) & 1;
         bw_arrive_warp(bar);
-        return bw_wait_warp(bar, parity, &s->stop);
+        return bw_wait_warp(bar, parity, &s->waits);
     }
     __device__ bool run(int n);
     __device__ bool finish(const Unit& u, float top, float sum, bool row, bool busy, int r);
@@ -679,9 +689,9 @@ __device__ __noinline__ bool clear_lines(Rest* s, const Sight& see, Border& b) {
     auto meet = [&](bool both) {
         const uint32_t bar = bw_smem(both ? &s->meet : &s->group_meet[b.w]), parity = (both ? b.meets++ : b.group_meets++) & 1;
         bw_arrive_warp(bar);
-        return bw_wait_warp(bar, parity, &s->stop);
+        return bw_wait_warp(bar, parity, &s->waits);
     };
-    if (!bw_wait_warp(b.v_full, b.v_parity, &s->stop)) return false;
+    if (!bw_wait_warp(b.v_full, b.v_parity, &s->waits)) return false;
     const uint32_t of_warp = lines_without_numbers<T, D>(b.values, b.t);
     if ((b.t & 31) == 0) s->lines[b.w][b.t >> 5] = of_warp;
     if (!meet(b.both)) return false;
@@ -727,7 +737,7 @@ __device__ bool Softmax<T, D>::run(int n) {
         const int k = k0 + (wide ? j >> 1 : j), number = k < sink_tiles ? k : k + behind;
         const bool masked = number >= plain_end || (number < plain_from && number >= sinks_end);
         if (wide && j == 0 && (masked || !busy)) bw_arrive_warp(bw_smem(&s->lead));     // (a border takes both groups)
-        if (!bw_wait_warp(bw_smem(&s->s_full[w]), s_count++ & 1, &s->stop)) return false;
+        if (!bw_wait_warp(bw_smem(&s->s_full[w]), s_count++ & 1, &s->waits)) return false;
         bw_fence_after();
         if (busy) {
             // 32 scores at a time, the next ones on their way; twice from tensor memory, for the maximum and for the weights (all in registers at once: spills, and
@@ -819,8 +829,8 @@ __device__ __forceinline__ bool Softmax<T, D>::finish(const Unit& u, float top, 
         s->sums[w][t] = make_float2(top, sum);
         if (!meet()) return false;
     }
-    if (!wide || w == 0) { if (!bw_wait_warp(bw_smem(&s->o_done[0]), o_count0 & 1, &s->stop)) return false; }
-    if (two || (wide && w == 1)) { if (!bw_wait_warp(bw_smem(&s->o_done[1]), o_count1 & 1, &s->stop)) return false; }
+    if (!wide || w == 0) { if (!bw_wait_warp(bw_smem(&s->o_done[0]), o_count0 & 1, &s->waits)) return false; }
+    if (two || (wide && w == 1)) { if (!bw_wait_warp(bw_smem(&s->o_done[1]), o_count1 & 1, &s->waits)) return false; }
     ++o_count0;
     o_count1 += wide || two;
     bw_fence_after();
@@ -899,7 +909,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
         for (int e = 0; e < UNITS; ++e) { bw_bar_init(bw_smem(&s->unit_full[e]), 1); bw_bar_init(bw_smem(&s->unit_empty[e]), 11); }
         bw_bar_init(bw_smem(&s->meet), 8);
         bw_bar_init(bw_smem(&s->lead), 4);
-        s->stop = 0; s->begun[0] = s->begun[1] = 0;
+        s->waits.stop = 0; s->waits.limit = a.limit; s->begun[0] = s->begun[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (t < CHUNKS) s->costs[t] = 0;
@@ -916,35 +926,31 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
     if (warp == 0 || warp == 2) {
         Lines<D> f = {a, warp ? &mv : &mk, s, ring, (uint32_t)warp >> 1, lane / S::HALVES, lane % S::HALVES, (uint32_t)warp >> 1};
         if (warp == 0) walk_units<D>(a, &mq, s, q, f, lane);
-        else {
-            copy_values<D>(f);
-            if (a.b.d_status) write_status(a, s, lane);
-        }
-    }
-    else if (warp == 1 || warp == 3) {
-        const int w = warp >> 1;
-        if (!multiply<T, D>(a, s, ring, q, tmem, w)) {
-            int never = 0;                                        // the products in flight come to their end
-            bw_commit(bw_smem(&s->over[w]), lane == 0);
-            bw_wait_slow(bw_smem(&s->over[w]), 0, &never, 200000000ll);
+        else copy_values<D>(f);
+    } else if (warp == 1 || warp == 3) {
+        const bool leader = bw_elect();
+        multiply<T, D>(a, s, ring, q, tmem, warp >> 1, leader);
+        if (all_through(s)) {
+            bw_commit(bw_smem(&s->over[warp >> 1]), leader);
+            bw_wait_end(bw_smem(&s->over[warp >> 1]), 0);
         }
     } else {
         const int row = (t - 128) & 127;
         Softmax<T, D> f = {a, s, smem, tmem + ((uint32_t)(warp & 3) << 21), (warp - 4) >> 2, row, row / a.group, row % a.group};
         for (int n = 0;; ++n) {
-            if (!bw_wait_warp(bw_smem(&s->unit_full[n % UNITS]), (n / UNITS) & 1, &s->stop)) break;
+            if (!bw_wait_warp(bw_smem(&s->unit_full[n % UNITS]), (n / UNITS) & 1, &s->waits)) break;
             if (!f.run(n)) break;
         }
+        all_through(s);
     }
     __syncwarp();
-    bw_fence_before();
-    __syncthreads();
+    if (s->waits.stop) __syncthreads();                           // (what was asked for has come to its end)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (from the begin on, the next kernel's waiting blocks cost small calls a quarter)
     if (warp == 1) {
         bw_fence_after();
         bw_tmem_free(tmem, 512);
     }
-    if (s->stop && a.b.d_status)                                  // given up
+    if (s->waits.stop && a.b.d_status)                            // given up
         for (int i = t; i < a.b.n; i += THREADS) atomicOr(&a.b.d_status[i], SD_STATUS_FAILED);
 }
 
@@ -1074,6 +1080,9 @@ __global__ void __launch_bounds__(256) join_planes_kernel(const __grid_constant_
 }
 
 // ---- host ----------------------------------------------------------------------------------
+constexpr long long WAIT_LIMIT = 4000000000;                      // two seconds
+std::atomic<long long> g_limit{0};                                // of sd_debug_attend_limit
+
 int check(const sd_cache* cache, const sd_rows* rows, const sd_attend_params* prm) {
     const int rc = sd_check_cache(cache, rows);
     if (rc != SD_OK) return rc;
@@ -1199,6 +1208,7 @@ extern "C" int sd_attend(const sd_cache* cache, const sd_rows* rows, const sd_at
     // (A factor of 0: the least number keeps scores that are not seen, -inf, what they are.)
     a.scale = std::max(std::abs(prm->scale) * 1.4426950408889634f, 1.17549435e-38f);
     a.box = std::min(cache->page_size, TILE);
+    a.limit = g_limit > 0 ? g_limit.load() : WAIT_LIMIT;
     a.cuts = (Cut*)(w + r.cuts); a.part = (float*)(w + r.part); a.part_lse = (float*)(w + r.part_lse);
     a.plane[0] = (float*)(w + r.plane); a.plane[1] = a.plane[0] + lines * cache->head_dim;
     a.plane_lse[0] = (float*)(w + r.plane_lse); a.plane_lse[1] = a.plane_lse[0] + lines;
@@ -1206,3 +1216,5 @@ extern "C" int sd_attend(const sd_cache* cache, const sd_rows* rows, const sd_at
     if (cache->dtype == SD_BF16) return cache->head_dim == 128 ? launch<__nv_bfloat16, 128>(a, r, st) : launch<__nv_bfloat16, 64>(a, r, st);
     return cache->head_dim == 128 ? launch<__half, 128>(a, r, st) : launch<__half, 64>(a, r, st);
 }
+
+extern "C" void sd_debug_attend_limit(int64_t cycles) { g_limit = cycles; }

@@ -1,7 +1,7 @@
 // Tensor memory, tensor-core products, tiled copies and barriers of sm_100a, as the PTX instructions that they are.
 //
-// Every wait has an end: where a barrier is not passed within 4e9 cycles (two seconds) the block's `stop` word is set, every other wait of
-// the block sees it, and the block winds up (see Waits).
+// Every wait has an end: where a barrier is not passed within some cycles (Waits::limit) the block's `stop` word is set, every other wait of
+// the block sees it, and the block winds up.  What it has in flight it waits for even then (bw_wait_end), before its memory is another's.
 #pragma once
 
 #include <cuda.h>
@@ -26,28 +26,30 @@ __device__ __forceinline__ bool bw_try(uint32_t bar, uint32_t parity) {
     return done;
 }
 
-// False: given up, here or elsewhere in the block.
-__device__ __noinline__ bool bw_wait_slow(uint32_t bar, uint32_t parity, volatile int* stop, long long limit) {
+// In shared memory, of a block: whether a wait was given up, and the cycles that one may take.
+struct Waits {
+    int stop;
+    long long limit;
+};
+
+// What is in flight comes to its end, or two hundred million cycles (a tenth of a second) pass: the block has given up already.
+__device__ __noinline__ void bw_wait_end(uint32_t bar, uint32_t parity) {
     const long long begin = clock64();
-    while (!bw_try(bar, parity)) {
-        if (*stop) return false;
-        if (clock64() - begin > limit) { *stop = 1; return false; }
-    }
-    return true;
+    while (!bw_try(bar, parity) && clock64() - begin <= 200000000ll) {}
 }
-// ... for a whole warp: all of its lanes go on or none does.  They come together first: lanes that wait may keep the others of their warp from running, so none of them may
-// still have something to do that the barrier waits for.
-__device__ __noinline__ bool bw_wait_slow_warp(uint32_t bar, uint32_t parity, volatile int* stop) {
-    const long long begin = clock64();
+// False: given up, here or elsewhere in the block.  For a whole warp: all of its lanes go on or none does.  They come together first: lanes that wait may keep the others
+// of their warp from running, so none of them may still have something to do that the barrier waits for.
+__device__ __noinline__ bool bw_wait_slow_warp(uint32_t bar, uint32_t parity, volatile Waits* w) {
+    const long long begin = clock64(), limit = w->limit;
     while (!__all_sync(~0u, bw_try(bar, parity))) {
-        if (__any_sync(~0u, *stop || clock64() - begin > 4000000000ll)) { *stop = 1; return false; }
+        if (__any_sync(~0u, w->stop || clock64() - begin > limit)) { w->stop = 1; return false; }
     }
     return true;
 }
-__device__ __forceinline__ bool bw_wait_warp(uint32_t bar, uint32_t parity, volatile int* stop) {
+__device__ __forceinline__ bool bw_wait_warp(uint32_t bar, uint32_t parity, volatile Waits* w) {
     __syncwarp();
     if (__all_sync(~0u, bw_try(bar, parity))) return true;
-    return bw_wait_slow_warp(bar, parity, stop);
+    return bw_wait_slow_warp(bar, parity, w);
 }
 
 __device__ __forceinline__ void bw_fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }   // plain writes before what the tensor cores and copies do
