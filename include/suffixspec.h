@@ -60,7 +60,7 @@ enum {
                                   /* length or its path make no sense; left out       */
     SD_STATUS_BAD_PAGE = 32,      /* a page outside the cache was met                 */
     SD_STATUS_FAILED = 64         /* sd_attend gave up waiting on the device: nothing */
-                                  /* of the call is of use                            */
+                                  /* of the call is of use (told to all requests)     */
 };
 
 /* sd_spec_params.flags */
@@ -376,6 +376,7 @@ int sd_rotate(const sd_cache* cache, const sd_rows* rows, const sd_rotate_params
  * each only if its position is inside the row's window or below `sinks`.  out = softmax(scale * q k) v over these;
  * 0 for a row that sees nothing.  Scores, softmax and sums are 32 bits; weights are rounded to the cache's type
  * for the product with the values.  What a row does not see has no part in its result, whatever it holds (NaN too).
+ * A call that gives up a wait on the device (after 4e9 cycles) tells every request SD_STATUS_FAILED, and leaves NaN in their rows of d_out and d_lse.
  *   d_q, d_out   [rows][q_heads][head_dim], by their strides; d_out may be d_q with the same strides
  *   d_lse        float[rows][q_heads] or NULL: log of the sum of exp(score), -inf for a row that sees nothing
  *   d_workspace  sd_attend_workspace() bytes, 256-byte aligned, undefined before and after; a call needs one of its own as long as it runs

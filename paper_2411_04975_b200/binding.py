@@ -22,7 +22,7 @@ from . import build as _build
 
 FLAG_GLOBAL_ONLY, FLAG_REQUEST_ONLY, FLAG_LINEAR = 1, 2, 4
 STATUS_BAD_SLOT, STATUS_POOL_FULL, STATUS_GLOBAL_FULL, STATUS_BAD_TOKEN = 1, 2, 4, 8
-STATUS_BAD_ROWS, STATUS_BAD_PAGE = 16, 32
+STATUS_BAD_ROWS, STATUS_BAD_PAGE, STATUS_FAILED = 16, 32, 64
 
 EXPORTS = ["sd_build", "sd_build_requests", "sd_append", "sd_speculate", "sd_step", "sd_speculate_noalloc", "sd_query_counts",
            "sd_enumerate", "sd_slot_info", "sd_entropy", "sd_stats", "sd_free", "sd_trim", "sd_strerror", "sd_debug_fail_alloc",

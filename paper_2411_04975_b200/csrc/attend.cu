@@ -63,6 +63,7 @@ struct AttendArgs {
     float scale;                  // of scores, for powers of two; not negative: the products turn the sign
     long long limit;              // cycles that a wait may take
     int box;                      // lines that one copy fetches
+    int* gave_up;                 // [grid]: whether block c has given up a wait
     Cut* cuts;                    // [grid]: the unit that begins in block c and is cut
     float* part;                  // [2 * grid][256][D]: packed rows of a cut unit; slot 2c: it came from the block before, 2c + 1: it goes on in the next
     float* part_lse;              // [2 * grid][256]
@@ -950,14 +951,38 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
         bw_fence_after();
         bw_tmem_free(tmem, 512);
     }
-    if (s->waits.stop && a.b.d_status)                            // given up
-        for (int i = t; i < a.b.n; i += THREADS) atomicOr(&a.b.d_status[i], SD_STATUS_FAILED);
+    if (t == 0) a.gave_up[blockIdx.x] = s->waits.stop;
 }
 
 // ---- joining -------------------------------------------------------------------------------
 // A warp per packed row of a cut unit: its parts by their sums.  Rows of few calls are many, so that what a row takes is the latency of its loads: the cut, then its
 // sums and eight parts at once (one token over a long context 23.5 -> 19.5 us against a kernel that first looked up where a row belongs and loaded parts behind the sums).
 constexpr int JOIN_ROWS = 8, JOIN_BLOCKS = 16, AHEAD = 8, MOST_BLOCKS = 1024;
+
+// By a whole block: has any of attend_kernel's given up?  (Told here, behind all of them, so that no block's status comes after it.)
+__device__ __forceinline__ bool any_gave_up(const AttendArgs& a, int blocks) {
+    bool any = false;
+    for (int e = threadIdx.x; e < blocks; e += blockDim.x) any |= a.gave_up[e] != 0;
+    return __syncthreads_or(any);
+}
+
+// Then all requests are told, and their rows say so too: a call need not ask for statuses.
+template <int D>
+__device__ __noinline__ void tell_given_up(const AttendArgs& a) {
+    const sd_rows& b = a.b;
+    constexpr int PER = D / 8;                                    // pieces of 16 bytes of a head
+    for (int i = blockIdx.x; i < b.n; i += gridDim.x) {
+        if (b.d_status && threadIdx.x == 0) b.d_status[i] |= SD_STATUS_FAILED;
+        const Request r = sd_request(b, i, a.c.page_size, a.p.shared);
+        for (int e = threadIdx.x; e < r.count * a.p.q_heads; e += blockDim.x) {
+            const long long row = r.begin + e / a.p.q_heads;
+            const int h = e % a.p.q_heads;
+            uint4* to = (uint4*)((uint16_t*)a.out + row * a.p.out_stride[0] + h * a.p.out_stride[1]);
+            for (int c = 0; c < PER; ++c) to[c] = make_uint4(0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu);   // (no number in either type)
+            if (a.lse) a.lse[row * a.p.q_heads + h] = NAN;
+        }
+    }
+}
 
 template <class T, int D>
 __device__ void join_row(const AttendArgs& a, const Cut& c, int m, int lane, bool planes) {
@@ -1032,6 +1057,7 @@ template <class T, int D>
 __global__ void __launch_bounds__(32 * JOIN_ROWS) join_cuts_kernel(const __grid_constant__ AttendArgs a, bool planes, int blocks) {
     sd_chain_begin();
     const Cut c = a.cuts[blockIdx.x % blocks];
+    if (any_gave_up(a, blocks)) { tell_given_up<D>(a); return; }
     if (c.last < c.first) return;
 #pragma unroll 1
     for (int m = blockIdx.x / blocks * JOIN_ROWS + (threadIdx.x >> 5); m < c.rows * a.group; m += gridDim.x / blocks * JOIN_ROWS) join_row<T, D>(a, c, m, threadIdx.x & 31, planes);
@@ -1039,8 +1065,9 @@ __global__ void __launch_bounds__(32 * JOIN_ROWS) join_cuts_kernel(const __grid_
 
 // With a shared prefix: it and what is behind it, a warp per row and head.
 template <class T, int D>
-__global__ void __launch_bounds__(256) join_planes_kernel(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(256) join_planes_kernel(const __grid_constant__ AttendArgs a, int blocks) {
     sd_chain_begin();
+    if (any_gave_up(a, blocks)) return;                           // (told already)
     constexpr int E = D / 32;
     const sd_rows& b = a.b;
     const int lane = threadIdx.x & 31;
@@ -1102,7 +1129,7 @@ int check(const sd_cache* cache, const sd_rows* rows, const sd_attend_params* pr
 struct Room {
     int blocks;
     bool planes;
-    int64_t cuts, part, part_lse, plane, plane_lse, all;          // bytes; begins of the parts
+    int64_t gave_up, cuts, part, part_lse, plane, plane_lse, all;          // bytes; begins of the parts
 };
 
 // Blocks and workspace of a call: as many blocks as multiprocessors, fewer where the longest lengths that the tables hold make less work than that.
@@ -1118,6 +1145,7 @@ int room_for(const sd_cache* c, const sd_rows* b, const sd_attend_params* p, Roo
     r->blocks = (int)std::max(1ll, std::min((long long)std::min(sms, MOST_BLOCKS), (units * (longest * WIDE + ENDS) + LEAST - 1) / LEAST));
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t was = at; at += (bytes + 255) / 256 * 256; return was; };
+    r->gave_up = take(r->blocks * (int64_t)sizeof(int));
     r->cuts = take(r->blocks * (int64_t)sizeof(Cut));
     r->part = take(2ll * r->blocks * 256 * c->head_dim * 4);
     r->part_lse = take(2ll * r->blocks * 256 * 4);
@@ -1174,7 +1202,7 @@ int launch(const AttendArgs& a, const Room& r, cudaStream_t st) {
     if (a.b.rows == 0) return SD_OK;
     const long long rows = std::min((long long)a.b.rows, 2ll * a.tile_rows) * a.group;  // packed ones of a cut
     SD_CUDA_OK(sd_launch(join_cuts_kernel<T, D>, r.blocks * (unsigned)std::min((rows + JOIN_ROWS - 1) / JOIN_ROWS, (long long)JOIN_BLOCKS), 32 * JOIN_ROWS, 0, st, a, r.planes, r.blocks));
-    if (r.planes) SD_CUDA_OK(sd_launch(join_planes_kernel<T, D>, a.b.rows, 256, 0, st, a));
+    if (r.planes) SD_CUDA_OK(sd_launch(join_planes_kernel<T, D>, a.b.rows, 256, 0, st, a, r.blocks));
     return SD_OK;
 }
 
@@ -1209,7 +1237,7 @@ extern "C" int sd_attend(const sd_cache* cache, const sd_rows* rows, const sd_at
     a.scale = std::max(std::abs(prm->scale) * 1.4426950408889634f, 1.17549435e-38f);
     a.box = std::min(cache->page_size, TILE);
     a.limit = g_limit > 0 ? g_limit.load() : WAIT_LIMIT;
-    a.cuts = (Cut*)(w + r.cuts); a.part = (float*)(w + r.part); a.part_lse = (float*)(w + r.part_lse);
+    a.gave_up = (int*)(w + r.gave_up); a.cuts = (Cut*)(w + r.cuts); a.part = (float*)(w + r.part); a.part_lse = (float*)(w + r.part_lse);
     a.plane[0] = (float*)(w + r.plane); a.plane[1] = a.plane[0] + lines * cache->head_dim;
     a.plane_lse[0] = (float*)(w + r.plane_lse); a.plane_lse[1] = a.plane_lse[0] + lines;
     cudaStream_t st = (cudaStream_t)stream;

@@ -58,3 +58,42 @@ def test_a_call_that_gives_up_waits_for_what_it_has_asked_for_and_for_no_more(li
         sfx.sd_attend(*a, mask=mask)
         torch.cuda.synchronize()
         assert time.monotonic() - begin < 0.08, cycles
+
+
+@pytest.mark.parametrize("name", BATCHES)
+def test_a_call_that_gives_up_says_so(name, limit):
+    """In every status, whichever block was the last, and in the rows, as statuses need not be asked for."""
+    args, kw = BATCHES[name]
+    b = R.Batch(args["contexts"], args["drafts"], **{k: v for k, v in args.items() if k not in ("contexts", "drafts")}, seed=92, extra_rows=2)
+    k, v = b.caches()
+    (table, offsets, cached), mask = b.args(), b.mask_arg()
+    bad = int(b.n > 1)
+    if bad:
+        cached[0] = -1                                            # (a request that makes no sense has its own status beside it)
+    heads, last, first = b.q.shape[1], int(b.offsets[-1]), int(b.offsets[bad])
+    wide = torch.empty(b.rows, heads + 1, b.head, dtype=b.dtype, device="cuda:0")
+    out, lse, status = wide[:, 1:], torch.empty(b.rows, heads, device="cuda:0"), torch.empty(b.n, dtype=torch.int32, device="cuda:0")
+
+    def run(cycles):
+        wide.fill_(7.0), lse.fill_(5.0), status.fill_(99)
+        limit(cycles)
+        sfx.sd_attend(b.q.cuda(), k, v, table, offsets, cached, mask=mask, out=out, lse=lse, status=status, **kw)
+        limit(0)
+        return status.tolist(), out.clone(), lse.clone()
+
+    sound = run(0)
+    assert sound[0] == [16] * bad + [0] * (b.n - bad)
+    seen = 0
+    for cycles in [1] * 20 + list(range(500, 20000, 250)):
+        got = run(cycles)
+        failed = got[0][0] & sfx.STATUS_FAILED
+        assert got[0] == [s | failed for s in sound[0]], cycles
+        seen += failed != 0
+        if failed:
+            assert torch.isnan(got[1][first:last]).all() and torch.isnan(got[2][first:last]).all()
+            for t, was in ((got[1], 7.0), (got[2], 5.0), (wide[:, :1], 7.0)):
+                assert (t[:first] == was).all() and (t[last:] == was).all()
+            assert (wide[:, 0] == 7.0).all()
+        else:
+            assert torch.equal(got[1], sound[1]) and torch.equal(got[2], sound[2])
+    assert seen >= 20
