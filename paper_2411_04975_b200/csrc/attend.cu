@@ -916,13 +916,13 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
     if (t < CHUNKS) s->costs[t] = 0;
     if (t == CHUNKS) { s->all = 0; s->some = 0x7FFFFFFF; s->end = 0; }
     if (t == 32 * 3) { bw_prefetch_map(&mk); bw_prefetch_map(&mv); bw_prefetch_map(&mq); }
-    if (warp == 1) bw_tmem_alloc(bw_smem(&s->tmem), 512);
+    __syncthreads();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (warp == 1) bw_tmem_alloc(bw_smem(&s->tmem), 512);         // (not before the wait: a kernel there, of another library, may still ask for some, and would wait for this one)
+    add_up(a, s, t);
     bw_fence_before();
     __syncthreads();
     bw_fence_after();
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    add_up(a, s, t);
-    __syncthreads();
     const uint32_t tmem = s->tmem, ring = bw_smem(smem + S::RING), q = bw_smem(smem + S::Q);
     if (warp == 0 || warp == 2) {
         Lines<D> f = {a, warp ? &mv : &mk, s, ring, (uint32_t)warp >> 1, lane / S::HALVES, lane % S::HALVES, (uint32_t)warp >> 1};

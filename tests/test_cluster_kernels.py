@@ -1,4 +1,5 @@
-"""Kernels of clusters, by their source: a block's shared memory is reached from another only behind a barrier of the cluster, before which nothing says that it has begun."""
+"""Orders that no run can show, by the sources.  A block's shared memory is reached from another only behind a barrier of the cluster, before which nothing says that it has begun;
+tensor memory is asked for when the kernel in front has ended."""
 import os
 import re
 
@@ -29,3 +30,10 @@ def test_blocks_of_a_cluster_are_there_before_their_memory_is_reached(body):
 
 def test_there_are_such_kernels():
     assert len(list(kernels())) >= 2
+
+
+def test_tensor_memory_is_asked_for_behind_the_kernel_before():
+    """Asked for while the kernel in front still runs, it could be what that kernel asks for next, and each would wait for the other."""
+    with open(os.path.join(build.CSRC, "attend.cu")) as h:
+        body = re.split(r"__global__", h.read())[1].split("\n}\n")[0]
+    assert body.index("griddepcontrol.wait") < body.index("bw_tmem_alloc(")
