@@ -118,6 +118,14 @@ def test_attend_many_requests():
     check_attend(R.Batch(rng.integers(0, 80, n).tolist(), rng.integers(-1, 4, n).tolist(), head=64, group=1, seed=11))
 
 
+@pytest.mark.parametrize("n", [2048, 2049, 2100, 4200])
+@pytest.mark.parametrize("shared,kw", [(0, {}), (128, dict(shared=128)), (0, dict(window=40, sinks=2))], ids=str)
+def test_attend_requests_by_more_than_32(n, shared, kw):
+    """Beyond 2,048 requests the pieces that the list is added up in have more than 32 requests each."""
+    rng = np.random.default_rng(1100 + n)
+    check_attend(R.Batch((shared + rng.integers(0, 40, n)).tolist(), rng.integers(-1, 3, n).tolist(), M=3, head=64, kv_heads=1, group=1, shared=shared, seed=n), **kw)
+
+
 def test_attend_empty_rows():
     """A draft node that does not see itself, whose ancestors and the last token are outside its window: nothing is left."""
     b = R.Batch([40, 300], [6, 6], seed=12)

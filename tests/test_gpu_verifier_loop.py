@@ -72,6 +72,53 @@ def test_steps_of_a_batch():
     store.free()
 
 
+def test_what_is_accepted_goes_to_the_next_step_as_it_is():
+    """sd_accept's offsets and tokens as sd_step's arguments, on the device, with a slot that idles in every other step; beside a store that is given the known tokens."""
+    w = get_workload("tiny")
+    c, n = w.cfg, 6
+    prompts = [w.prompt(i) for i in range(n)]
+    truth = [w.continuation(i, prompts[i], length=120) for i in range(n)]
+    off = np.concatenate([[0], np.cumsum([len(p) for p in prompts])])
+    slots = torch.arange(n, dtype=torch.int32, device=DEV)
+    stores = [store_of(w, n, 250) for _ in range(2)]
+    for store in stores:
+        store.build_requests(list(range(n)), off, torch.as_tensor(np.concatenate(prompts).astype(np.int32), device=DEV))
+    args = (c.max_pattern, c.alpha, c.max_spec)
+    out = stores[0].speculate(slots, *args)
+    cursor, accepted = [0] * n, 0
+    for turn in range(8):
+        idle = turn % n if turn % 2 else -1
+        drafts = out["n_draft"].cpu().numpy()
+        counts = [0 if i == idle else 1 + int(drafts[i]) for i in range(n)]
+        offsets = np.concatenate([[0], np.cumsum(counts)])
+        tokens, parents = out["tokens"].cpu().numpy(), out["parents"].cpu().numpy()
+        positions = out["positions"].cpu().numpy()
+        logits = torch.randn(int(offsets[-1]) + 3, c.vocab, generator=torch.Generator().manual_seed(turn))
+        for i in range(n):
+            for r in range(counts[i]):                            # the model's choice at a row is the token that follows its position
+                depth = 0 if r == 0 else int(positions[i, r - 1]) - (len(prompts[i]) + cursor[i]) + 1
+                logits[int(offsets[i]) + r, int(truth[i][cursor[i] + depth])] = 50.0
+        got = sfx.sd_accept(logits.cuda(), torch.as_tensor(offsets, device=DEV), out["tokens"], out["parents"])
+        out = stores[0].step(slots, got["offsets"], got["tokens"], *args)
+        known = []
+        for i in range(n):
+            many = 0 if i == idle else 1 + accept_longest_path(tokens[i], parents[i], int(drafts[i]), truth[i][cursor[i]:])
+            known.append(truth[i][cursor[i]:cursor[i] + many])
+            cursor[i] += many
+            accepted += max(many - 1, 0)
+        begin = np.concatenate([[0], np.cumsum([len(t) for t in known])])
+        assert got["offsets"].tolist() == begin.tolist() and got["tokens"].tolist() == np.concatenate(known).tolist() + [-1] * (len(logits) - int(begin[-1]))
+        stores[1].append(slots, torch.as_tensor(begin, device=DEV), torch.as_tensor(np.concatenate(known).astype(np.int32), device=DEV))
+        want = stores[1].speculate(slots, *args)
+        for name in ("n_draft", "tokens", "parents", "positions", "mask", "chosen_tree", "chosen_p", "score", "status"):
+            assert torch.equal(out[name], want[name]), name
+        if max(cursor) > 60:
+            break
+    assert accepted > n
+    for store in stores:
+        store.free()
+
+
 def test_a_step_in_a_graph_with_idle_slots():
     """One captured step of the verifier's calls, replayed with other drafts; slots without rows and room behind the rows."""
     from verifier_ref import Batch, accept, attend, rotate
