@@ -475,8 +475,8 @@ __device__ __forceinline__ int uniform(int x) { return __shfl_sync(~0u, x, 0); }
 template <class T, int D>
 __device__ void multiply(const AttendArgs& a, Rest* s, uint32_t ring, uint32_t q, uint32_t tmem_, int w, bool leader) {
     using S = Shape<D>;
-    const uint32_t qk = bw_idesc(IsBf16<T>::v, 128, TILE, false) | (a.p.scale < 0.f ? 1u << 13 : 0u);   // (negated queries)
-    constexpr uint32_t pv = bw_idesc(IsBf16<T>::v, 128, D, true);
+    const uint32_t qk = bw_idesc(IsBf16<T>::v, 128, TILE, false, a.p.scale < 0.f);
+    constexpr uint32_t pv = bw_idesc(IsBf16<T>::v, 128, D, true, false);
     const uint32_t tmem = uniform(tmem_), S0 = tmem + w * TILE, O0 = tmem + 2 * TILE + w * TILE;
     uint32_t it = 0, qi = 0, count = 0, wides = 0;                // slots, queries, jobs, wide units behind
     for (int n = 0;; ++n) {

@@ -73,8 +73,7 @@ __device__ __forceinline__ void bw_tmem_alloc(uint32_t where, uint32_t columns) 
 __device__ __forceinline__ void bw_tmem_free(uint32_t at, uint32_t columns) { asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory"); }
 __device__ __forceinline__ void bw_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void bw_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void bw_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-// ... and what was loaded is there: nothing that uses it is moved before the wait.
+// What was loaded is there: nothing that uses it is moved before the wait.
 __device__ __forceinline__ void bw_wait_ld32(uint32_t* r) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), 
@@ -139,8 +138,8 @@ __device__ __forceinline__ uint64_t bw_desc(uint32_t addr) {                    
 __device__ __forceinline__ uint64_t bw_desc_across(uint32_t addr, uint32_t next) {
     return (uint64_t)(addr >> 4) | (uint64_t)(next >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
-// 16-bit operands (bf16 or fp16, both alike), 32-bit sums, M rows and N columns.
-__device__ __forceinline__ constexpr uint32_t bw_idesc(bool bf16, int M, int N, bool b_across, bool minus_a = false) {
+// 16-bit operands (bf16 or fp16, both alike), 32-bit sums, M rows and N columns; `minus_a`: of the first operand negated.
+__device__ __forceinline__ constexpr uint32_t bw_idesc(bool bf16, int M, int N, bool b_across, bool minus_a) {
     return 1u << 4 | (minus_a ? 1u << 13 : 0u) | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (b_across ? 1u << 16 : 0u) | (uint32_t)(N >> 3) << 17 | (uint32_t)(M >> 4) << 24;
 }
 // Called by a whole warp that stays together (so that operands are computed once for it); `leader`: one of its lanes, which issues.
