@@ -454,7 +454,7 @@ def rotary_frequencies(rot_dim: int, base: float = 10000.0, *, device=None, fact
     """(freq, scale) for sd_rotate: base ** (-2 j / rot_dim) radians per position for pair j.  For contexts longer than a model was trained with,
     `factor` times as long: all frequencies divided by `factor` (original = 0), or, with `original` the length it was trained with, only
     those that turn less than `slow` times within it, none of those that turn more than `fast` times, the others in between in proportion
-    (linear in j), and the turned elements times 1 + 0.1 ln(factor)."""
+    (linear in j), and the turned elements times 1 + 0.1 ln(factor): the method "YaRN" of Peng et al. (arXiv 2309.00071), with its constants."""
     j = torch.arange(rot_dim // 2, dtype=torch.float64)
     freq = base ** (-2.0 * j / rot_dim)
     scale = 1.0

@@ -19,12 +19,13 @@
 //
 // What bounds it (bf16, 32 query heads on 8 heads of the cache of 128 elements where nothing else is said; microseconds of a call with its joins, and what the bytes or
 // products that it cannot do without would take of that at the measured 6.55 TB/s or 1,625 TFLOP/s):
-//   one token, 8,191 places               19.5   26 %: launches, code fetched for the first time, one chain copy - products - softmax - products, the join
-//   16 requests, 32 .. 400 places         22.5   11 %: the same (fp16, 16 heads of 64, drafts of up to 32)
+//   one token, 8,191 places               20     26 %: launches, code fetched for the first time, one chain copy - products - softmax - products, the join
+//                                                (18.9 in a graph, so the host is not what bounds it)
+//   16 requests, 32 .. 400 places         23     10 %: the same (fp16, 16 heads of 64, drafts of up to 32): 256 units on 148 multiprocessors, some 11 us of units' ends
 //   a draft of 24, 131,072 places        135     61 %: copies in the middle, the same begin and end around it
-//   64 requests, 1,000 .. 8,192 places   350     54 %: tiles of 256 rows take 3,800 cycles (products 2,050 of them; a group's chain of scores, maximum, weights, product
+//   64 requests, 1,000 .. 8,192 places   348     54 %: tiles of 256 rows take 3,800 cycles (products 2,050 of them; a group's chain of scores, maximum, weights, product
 //                                                is longer than what the other group and the tensor cores need meanwhile), units' ends 12,000 cycles each
-//   128 requests, window of 1,024        200     43 %: units' ends and the two tiles at the window's edges, which take five times as long as whole ones
+//   128 requests, window of 1,024     201 - 210  41 %: units' ends and the two tiles at the window's edges, which take five times as long as whole ones
 //   256 requests, 4,096 places shared    405     26 % of the products: tiles as above, 32-bit planes of both parts and their join (18)
 #include "blackwell.cuh"
 #include "verify.cuh"
@@ -956,7 +957,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_kernel(const __grid_constan
 
 // ---- joining -------------------------------------------------------------------------------
 // A warp per packed row of a cut unit: its parts by their sums.  Rows of few calls are many, so that what a row takes is the latency of its loads: the cut, then its
-// sums and eight parts at once (one token over a long context 23.5 -> 19.5 us against a kernel that first looked up where a row belongs and loaded parts behind the sums).
+// sums and eight parts at once (one token over a long context 23.5 -> 19.5 us against a kernel that first looked up where a row belongs and loaded parts behind the sums; 20 since it asks
+// first whether a block has given up).
 constexpr int JOIN_ROWS = 8, JOIN_BLOCKS = 16, AHEAD = 8, MOST_BLOCKS = 1024;
 
 // By a whole block: has any of attend_kernel's given up?  (Told here, behind all of them, so that no block's status comes after it.)

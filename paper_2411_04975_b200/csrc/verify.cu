@@ -11,10 +11,11 @@ namespace {
 // A block takes a few rows of one request (one, where there are few; ROT_ROWS in a large batch), so that what it looks up - where the rows are, how deep,
 // in which page - is two reads behind one another for all of them.  A row's heads go to the lanes of one or more warps, head_dim / 8 lanes a head and eight
 // elements a lane, always the same eight: what they are multiplied by (cosine, sine and weight in one factor for the element and one for the other of its
-// pair) stays in registers for all heads.  (Factors read from shared memory for every head, and pairs exchanged in 32 bits, took 400
+// pair) is kept for all heads: in registers, but for some 22 words of a thread, which six blocks a multiprocessor (80 registers) leave no room for.  (Factors read from shared memory for every head, and pairs exchanged in 32 bits, took 400
 // instructions for 256 elements and 69 us for 256 requests of up to 65 rows, now 33, 4.3 of the 6.55 TB/s that a
 // copy reaches.)  x' = x w / sqrt(mean(x^2) + eps) has its factor at the end, behind the turn, which is linear: y = (x_a m + x_b o) / sqrt(...).  Bound by the bytes of the
-// rows, every element is read once and written once; one request (5.6 us): by the launch and three reads behind one another.
+// rows, every element is read once and written once; one request (5.2 - 5.6 us): by the host, whose call takes as
+// long (3.5 in a graph: the launch and three reads behind one another).
 constexpr int ROT_THREADS = 128, ROT_WARPS = ROT_THREADS / 32;
 constexpr int ROT_ROWS = 4;
 constexpr int ROT_BATCH = 4;                                      // pieces that a lane has under way
@@ -177,8 +178,8 @@ __global__ void __launch_bounds__(ROT_THREADS, 6) rotate_kernel(const __grid_con
 // ---- sd_accept -----------------------------------------------------------------------------
 // The largest logit of a row, by a block.  The row is cut into chunks of 16 bytes (the first and the last may be shorter: a
 // row starts anywhere); a thread keeps the largest value it has seen and the chunk it was in, and only the winner's chunk is read
-// again for the place.  Bound by reading the logits: 256 requests' rows of 128,256 bf16 numbers 215 us, 6.8 TB/s (reads alone are faster than a copy); one request 10.6 us, of which
-// 5 are the second launch, which walks the tree.
+// again for the place.  Bound by reading the logits: 256 requests' rows of 128,256 bf16 numbers 219 us, 6.7 TB/s (reads alone are faster than a copy); one request 9.6 - 10.6 us, the host's
+// time for two launches (6.0 in a graph).
 constexpr int MAX_THREADS = 512;
 
 template <class T> __device__ __forceinline__ float as_float(T v);
@@ -387,7 +388,9 @@ __global__ void __launch_bounds__(WALK_THREADS) walk_kernel(const WalkArgs a) {
 // ---- sd_commit -----------------------------------------------------------------------------
 // A cluster per request, whose blocks take the planes (keys or values of a layer) in turns; a thread per 16 bytes of a line.  Lines only move to smaller
 // places, and a path ascends: what a batch of lines overwrites, no later batch reads.  The new length is written when all blocks have read the old one, which
-// may be the same memory.  Bound by the lines moved: 256 requests, 32 layers, 8 heads of 128: 22.6 us; one request 5.1 us, the launch and path, table and line behind one another.
+// may be the same memory.  256 requests, 32 layers, 8 heads of 128: 25 - 27 us; the 225 - 271 lines of them that move
+// (100 requests move any) are 59 - 71 MB, 9 - 11 us of the memory's time: a thread has the two or three lines of one request and plane under way, one plane after another.  One request
+// 4.6 - 5.1 us, the host's time (1.4 in a graph: path, table and line behind one another).
 constexpr int COMMIT_BATCH = 4, COMMIT_THREADS = 256;
 
 struct CommitArgs {
