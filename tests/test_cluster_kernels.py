@@ -22,7 +22,7 @@ def kernels():
                     yield pytest.param(body, id=f + ":" + re.search(r"(\w+_kernel)\(", body).group(1))
 
 
-@pytest.mark.parametrize("body", kernels())
+@pytest.mark.parametrize("body", list(kernels()))
 def test_blocks_of_a_cluster_are_there_before_their_memory_is_reached(body):
     barrier = BARRIER.search(body)
     assert barrier and barrier.start() < body.index("map_shared_rank")
